@@ -405,6 +405,84 @@ size_t zsa_decode_workspace_size(const zsa_layer_cfg* cfg, int32_t n_layers, int
                                  int32_t kv_capacity);
 
 /* ---------------------------------------------------------------------
+ * A key/value cache in pages, for one layer. Pruning leaves every layer
+ * another number of rows per sequence, and generation adds to them: pages
+ * of a pool, named by a table, hold them without a slab sized for the
+ * longest.
+ *   pool       [n_pages] pages of page_size rows [k | v], dtype, device;
+ *              page p starts at p * page_stride elements; a row is
+ *              2 * n_kv_heads * head_dim elements, k in the first half
+ *   table      [batch, table_stride] int32 device: row r of sequence b is
+ *              row r % page_size of page table[b][r / page_size]; a row of
+ *              the table holds max_pages ids
+ *   page_size  a power of two from 16 on
+ * Entries beyond a sequence's rows are not used. A page id outside
+ * [0, n_pages) reads as a page of zeros, and what is stored there is lost.
+ */
+typedef struct zsa_paged_kv {
+  void* pool;
+  const int32_t* table;
+  int64_t page_stride, table_stride; /* elements, ids */
+  int32_t n_pages, page_size, max_pages;
+  int32_t n_kv_heads, head_dim, dtype;
+} zsa_paged_kv;
+
+/* Appends the new rows of every sequence to its cached ones, the keys
+ * rotated on the way (as ZSA_EPI_ROPE does).
+ *   k, v    row r starts at k + r * k_stride, v + r * v_stride (so that
+ *           both may lie in a fused projection's rows)
+ *   kv_len  [batch] int32 device: the sequence's rows with the new ones:
+ *           the new row r of n goes to cached row kv_len - n + r (one
+ *           below 0 or beyond the table is not stored)
+ *   pos     [T] int32 device: the rows' positions; NULL: stored as they are
+ *   q       NULL, or the same rows' queries, n_heads heads: rotated to q_out
+ *           (which may be q itself)
+ * No two of a call's rows may go to one cached row. T = 0 launches nothing.
+ */
+int zsa_paged_append(void* stream, const zsa_paged_kv* kv, const void* k, int64_t k_stride,
+                     const void* v, int64_t v_stride, const void* q, int64_t q_stride,
+                     int32_t n_heads, void* q_out, int64_t q_out_stride, const int32_t* pos,
+                     float rope_theta, int32_t batch, const int32_t* cu_host,
+                     const int32_t* cu_dev, const int32_t* kv_len);
+
+/* Attention (Eq. 1) of the new rows over the cached ones, theirs included:
+ * any number of new rows per sequence, one in generation.
+ *   q        row r of head h at q + r * q_stride + h * head_dim; head h
+ *            reads key/value head h / (n_heads / n_kv_heads)
+ *   causal   new row r of n sees the cached rows up to kv_len - n + r,
+ *            itself; else all kv_len. A row that sees none: out 0, lse -inf
+ *   kv_len   [batch] int32 device. Only the device knows it: a captured call
+ *            may be replayed with other values
+ *   max_kv_len  at least the largest kv_len (rows from it on are not read),
+ *            at most the table's rows
+ *   out      [T, n_heads*head_dim], row stride out_stride; lse [n_heads, T]
+ *            fp32 or NULL
+ *   ws >= zsa_paged_attention_workspace_size(..., prefix_len 0)
+ * bf16 or fp32, sums and softmax in fp32; head_dim 16, 32, 64 or 128.
+ */
+int zsa_paged_attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride,
+                        int32_t n_heads, int32_t causal, float scale, int32_t batch,
+                        const int32_t* cu_host, const int32_t* cu_dev, const int32_t* kv_len,
+                        int32_t max_kv_len, void* out, int64_t out_stride, float* lse, void* ws,
+                        size_t ws_bytes);
+
+/* The same for sequences that share their first prefix_len rows: those are
+ * cached once, in the pages prefix_pages [ceil(prefix_len / page_size)] int32
+ * device, come before each sequence's own rows (table, kv_len and max_kv_len:
+ * without them) and are seen by every new row. They are read once for the
+ * whole batch. prefix_len 0 is zsa_paged_attention. */
+int zsa_prefix_attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride,
+                         int32_t n_heads, int32_t causal, float scale, int32_t batch,
+                         const int32_t* cu_host, const int32_t* cu_dev, const int32_t* kv_len,
+                         int32_t max_kv_len, const int32_t* prefix_pages, int32_t prefix_len,
+                         void* out, int64_t out_stride, float* lse, void* ws, size_t ws_bytes);
+
+/* Bytes of workspace of both (0: none), for the current device. */
+size_t zsa_paged_attention_workspace_size(const zsa_paged_kv* kv, int32_t n_heads, int32_t batch,
+                                          const int32_t* cu_host, int32_t max_kv_len,
+                                          int32_t prefix_len);
+
+/* ---------------------------------------------------------------------
  * Timing hook (profiling aid, not thread-safe): while armed, the next
  * `capacity` kernel launches of class `kclass` are bracketed by HIP
  * start/stop events on their own stream. zsa_timing_read synchronises

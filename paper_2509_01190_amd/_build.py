@@ -22,6 +22,7 @@ LIB_PATH = os.path.join(HERE, "libzsa.so")
 SOURCES = [
     "zsa_api.cpp",
     "zsa_static.cpp",
+    "zsa_paged.cpp",
     "k_norm.hip",
     "k_gemm.hip",
     "k_attn.hip",
@@ -29,6 +30,7 @@ SOURCES = [
     "k_select.hip",
     "k_gather.hip",
     "k_decode.hip",
+    "k_paged.hip",
     "k_backward.hip",
     "k_wgrad.hip",
 ]
@@ -60,6 +62,7 @@ EXTRA_FLAGS = {
     "k_score.hip": VGPR_MFMA,
     "k_backward.hip": VGPR_MFMA,
     "k_decode.hip": VGPR_MFMA,
+    "k_paged.hip": VGPR_MFMA,
     "k_wgrad.hip": VGPR_MFMA,
 }
 

@@ -1,0 +1,412 @@
+// The key/value cache in pages: rows appended to it (with the rotary
+// embedding), the attention of new rows over a sequence's cached ones, and
+// the same where all sequences of a batch share their first rows.
+//
+// Layout: a pool of pages, each of page_size (a power of two, from 16 on) rows
+// [k | v], kvd = kv_heads * head_dim elements each; row r of sequence b is row
+// r % page_size of page table[b][r / page_size]. A page id outside the pool
+// stands for a page of zeros, and nothing is written to it.
+//
+//   append:    x'_i = x_i cos - x_{i + hd/2} sin, x'_{i + hd/2} = x_{i + hd/2} cos + x_i sin
+//              with the angle pos theta^(-2i/hd), for k and q; v as it is
+//   attention: s_j = scale q . k_j for the keys j that the row sees,
+//              out = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse = log sum_j exp(s_j);
+//              a row that sees no key: out = 0, lse = -inf
+//
+// New row r of sequence b, of its n, is the cached row len - n + r; under the
+// causal mask it sees the rows up to itself, else all len.
+#include <math.h>
+
+#include <algorithm>
+
+#include "zsa_internal.h"
+
+namespace zsa {
+namespace {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+// ---------------------------------------------------------------------------
+// append
+// ---------------------------------------------------------------------------
+constexpr int kAppendRows = 8;  // most rows of a workgroup
+
+// sequence of row t: cu[b] <= t < cu[b + 1] (t below cu[B]). One row per
+// sequence, as in generation, needs no search.
+__device__ __forceinline__ int sequence_of(const int32_t* __restrict__ cu, int B, int t) {
+  if (t < B && cu[t] <= t && t < cu[t + 1]) return t;
+  int lo = 0, hi = B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (t < cu[mid + 1])
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return lo;
+}
+
+// A workgroup takes `rows` rows: where each goes and its angles' (cos, sin) are
+// found once for all its heads, then every thread moves 16 bytes at a time (a
+// rotation's two halves together). Bound by the bytes: every row is read and
+// written once.
+template <typename T>
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, int rows) {
+  constexpr int V = Vec16<T>::N;
+  __shared__ float2 cs[kAppendRows][kMaxHalfHead];
+  __shared__ int64_t dst[kAppendRows];  // element in the pool, or -1
+  const int t0 = blockIdx.x * rows, nt = min(rows, a.T - t0);
+  const int tid = threadIdx.x, half = a.hd / 2;
+  if (tid < nt) {
+    const int t = t0 + tid, b = sequence_of(a.cu, a.B, t);
+    const int lo = a.cu[b], n = a.cu[b + 1] - lo;
+    const int64_t row = static_cast<int64_t>(a.kv_len[b]) - n + (t - lo);
+    int64_t d = -1;
+    if (row >= 0 && (row >> a.at.shift) < a.at.max_pages) {
+      const int page = a.at.table[b * a.at.table_stride + (row >> a.at.shift)];
+      if (page >= 0 && page < a.at.n_pages)
+        d = page * a.at.page_stride + (row & ((1 << a.at.shift) - 1)) * 2 * a.at.kvd;
+    }
+    dst[tid] = d;
+  }
+  if (a.pos != nullptr)
+    for (int i = tid; i < nt * half; i += 256) {
+      float s, c;
+      rope_angle(a.pos[t0 + i / half], a.inv_freq[i % half], &s, &c);
+      cs[i / half][i % half] = make_float2(c, s);
+    }
+  __syncthreads();
+  // a row's items: pairs of 16 bytes of the rotated heads, then 16 bytes of the others
+  const int hc = half / V, nq = a.q != nullptr ? a.H * hc : 0;
+  const int nrot = a.pos != nullptr ? nq + a.Hkv * hc : 0;
+  const int nk = a.pos != nullptr ? 0 : a.at.kvd / V, items = nrot + nk + a.at.kvd / V;
+  T* pool = static_cast<T*>(a.at.pool);
+  for (int i = tid; i < nt * items; i += 256) {
+    const int r = i / items, e = i - r * items;
+    const int64_t t = t0 + r, d = dst[r];
+    if (e < nrot) {
+      const bool isq = e < nq;
+      const int f = isq ? e : e - nq, h = f / hc, c = (f - h * hc) * V;
+      if (!isq && d < 0) continue;
+      const T* src = (isq ? static_cast<const T*>(a.q) + t * a.q_stride : static_cast<const T*>(a.k) + t * a.k_stride) + h * a.hd + c;
+      T* to = (isq ? static_cast<T*>(a.q_out) + t * a.q_out_stride : pool + d) + h * a.hd + c;
+      float x0[V], x1[V], y0[V], y1[V];
+      unpack16(*reinterpret_cast<const uint4*>(src), x0, T());
+      unpack16(*reinterpret_cast<const uint4*>(src + half), x1, T());
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float2 w = cs[r][c + j];
+        y0[j] = fmaf(x0[j], w.x, -(x1[j] * w.y));
+        y1[j] = fmaf(x1[j], w.x, x0[j] * w.y);
+      }
+      *reinterpret_cast<uint4*>(to) = pack16(y0, T());
+      *reinterpret_cast<uint4*>(to + half) = pack16(y1, T());
+    } else if (d >= 0) {
+      const int f = e - nrot;
+      const bool isk = f < nk;
+      const int c = (isk ? f : f - nk) * V;
+      const T* src = isk ? static_cast<const T*>(a.k) + t * a.k_stride + c : static_cast<const T*>(a.v) + t * a.v_stride + c;
+      *reinterpret_cast<uint4*>(pool + d + (isk ? 0 : a.at.kvd) + c) = *reinterpret_cast<const uint4*>(src);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------
+struct Span {     // what a workgroup works on
+  int lo;         // first row of the sequence, in the packed batch
+  int rows;       // its packed rows (new rows * G)
+  int len;        // cached rows that can be read
+  int first;      // keys that new row 0 sees under the mask: row r sees first + r (below len)
+  const int32_t* table;
+};
+
+__device__ __forceinline__ Span span_of(const PagedAttention& a, int b) {
+  Span s;
+  s.lo = a.cu != nullptr ? a.cu[b] : 0;
+  const int n = a.cu != nullptr ? a.cu[b + 1] - s.lo : a.T;
+  const int len = a.kv_len != nullptr ? max(a.kv_len[b], 0) : a.max_len;
+  s.rows = n * a.G;
+  s.len = static_cast<int>(min(static_cast<int64_t>(min(len, a.max_len)),
+                               static_cast<int64_t>(a.at.max_pages) << a.at.shift));
+  s.first = len - n + 1;
+  s.table = a.at.table + (a.cu != nullptr ? b * a.at.table_stride : 0);
+  return s;
+}
+
+// fp32 storage, and bf16 at head dims 16 and 32: both products on
+// v_mfma_f32_32x32x2_f32, fp32 operands and sums (the layout is that of the
+// fp32 attention over packed rows, k_attn.hip). One workgroup of four waves
+// per (split of the keys, 32 packed rows, key/value head, sequence); the waves
+// take the split's 32-key tiles in turn and their (max, sum, O) are merged
+// through LDS in wave order.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void paged_f32_kernel(PagedAttention a, int tiles, int splits) {
+  constexpr int NW = 4, KK = HD / 8;
+  constexpr int CT = HD < 32 ? 1 : HD / 32;  // 32-channel blocks of O (half empty at HD 16)
+  constexpr int HP = 33;                     // merge row stride: [channel][query]
+  __shared__ float so[NW][HD * HP];
+  __shared__ float sm[NW][32], sl[NW][32];
+  const int split = blockIdx.x % splits, it0 = blockIdx.x / splits;
+  const int tile = it0 % tiles, gb = it0 / tiles, g = gb % (a.H / a.G), b = gb / (a.H / a.G);
+  const Span sp = span_of(a, b);
+  const int i0 = tile * 32;
+  if (i0 >= sp.rows) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int half = lane >> 5, l32 = lane & 31;
+  const int row = min(i0 + l32, sp.rows - 1);  // rows past the sequence are not stored
+  const int lim = a.causal ? min(sp.first + row / a.G, sp.len) : sp.len;
+  const int lim0 = a.causal ? min(sp.first + i0 / a.G, sp.len) : sp.len;  // the tile's first row's
+  const int last = a.causal ? min(sp.first + min(i0 + 31, sp.rows - 1) / a.G, sp.len) : sp.len;
+  const int k0 = split * a.chunk, kend = min(last, k0 + a.chunk);
+  const int rs = 2 * a.at.kvd;
+  const T* pool = static_cast<const T*>(a.at.pool);
+  const T* qp = static_cast<const T*>(a.q) + static_cast<int64_t>(sp.lo + row / a.G) * a.q_stride + (g * a.G + row % a.G) * HD;
+  const bool vch = HD >= 32 || l32 < HD;  // lanes whose channel exists
+  float4 qf[KK];
+#pragma unroll
+  for (int s = 0; s < KK; ++s) qf[s] = load4<T>(qp + 8 * s + 4 * half);
+  float m_run = -INFINITY, l_run = 0.f;  // of the scaled scores; l_run: this lane's keys only
+  f32x16_t o[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
+  for (int j0 = k0 + wave * 32; j0 < kend; j0 += 32 * NW) {
+    // a page holds 16 rows at least: two of them here
+    const T* base[2];
+    bool there[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int j = j0 + 16 * i;
+      const int page = j < sp.len ? sp.table[j >> a.at.shift] : -1;
+      there[i] = page >= 0 && page < a.at.n_pages;
+      base[i] = pool + (there[i] ? page : 0) * a.at.page_stride +
+                static_cast<int64_t>(j & ((1 << a.at.shift) - 1)) * rs + g * HD;
+    }
+    float vr[CT][16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      // rows past the sequence count as zeros (their probability is 0)
+      const int jj = 8 * (r >> 2) + 4 * half + (r & 3), i = r >> 3;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+        vr[ct][r] = there[i] && j0 + jj < sp.len && vch
+                        ? to_f32(base[i][(jj & 15) * rs + a.at.kvd + ct * 32 + (HD < 32 ? l32 % HD : l32)])
+                        : 0.f;
+    }
+    f32x16_t s = {};
+    const bool kin = there[l32 >> 4] && j0 + l32 < sp.len;
+    const T* kp = (l32 >> 4 ? base[1] : base[0]) + (l32 & 15) * rs + 4 * half;
+#pragma unroll
+    for (int t = 0; t < KK; ++t) {
+      const float4 k4 = kin ? load4<T>(kp + 8 * t) : make_float4(0.f, 0.f, 0.f, 0.f);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, qf[t].x, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, qf[t].y, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.z, qf[t].z, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.w, qf[t].w, s, 0, 0, 0);
+    }
+    // s[r]: key j0 + 8 (r/4) + 4 half + r%4, query row
+    const bool edge = j0 + 32 > lim0;
+    float mloc = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int j = j0 + 8 * (r >> 2) + 4 * half + (r & 3);
+      s[r] = edge && j >= lim ? -INFINITY : s[r] * a.scale;
+      mloc = fmaxf(mloc, s[r]);
+    }
+    mloc = half_swap_max(mloc);
+    const float m_new = fmaxf(m_run, mloc);
+    if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {
+      const float alpha = m_new == -INFINITY ? 1.0f : expf(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
+      m_run = m_new;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = expf(s[r] - m_use);
+      l_run += s[r];
+    }
+    // A masked key's V row must not reach a query that does not see it, also
+    // where it holds an infinity or a NaN, which a product with its zero
+    // probability would spread. Such rows are rare: the tile then goes
+    // through the vector ALU, key by key.
+    bool odd = false;
+    if (edge) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) odd |= !(fabsf(vr[ct][r]) <= 3.402823466e38f);
+      odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+    }
+    if (!odd) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          o[ct] = __builtin_amdgcn_mfma_f32_32x32x2f32(vr[ct][r], s[r], o[ct], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < 32; ++kk) {
+        // key j0 + kk: register (kk / 8) * 4 + kk % 4 of lane half (kk / 4) % 2
+        const float p = __shfl(s[(kk >> 3) * 4 + (kk & 3)], l32 + 32 * ((kk >> 2) & 1), 64);
+        if (j0 + kk < lim && there[kk >> 4]) {
+          const T* vp = base[kk >> 4] + (kk & 15) * rs + a.at.kvd;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int c = ct * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+              if (c < HD) o[ct][r] = fmaf(p, to_f32(vp[c]), o[ct][r]);
+            }
+        }
+      }
+    }
+  }
+  l_run = half_swap_sum(l_run);
+  if (half == 0) {
+    sm[wave][l32] = m_run;
+    sl[wave][l32] = l_run;
+  }
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int c = ct * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+      if (c < HD) so[wave][c * HP + l32] = o[ct][r];
+    }
+  __syncthreads();
+  for (int it = tid; it < 32 * (HD / 4); it += 64 * NW) {
+    const int q = it / (HD / 4), c0 = (it % (HD / 4)) * 4, i = i0 + q;
+    if (i >= sp.rows) continue;
+    float m = sm[0][q];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, sm[w][q]);
+    float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      // a wave without keys for this query holds the empty sum
+      if (sm[w][q] == -INFINITY && sl[w][q] == 0.f) continue;
+      const float f = expf(sm[w][q] - (m == -INFINITY ? 0.f : m));
+      l = fmaf(f, sl[w][q], l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(f, so[w][(c0 + e) * HP + q], v[e]);
+    }
+    const int t = sp.lo + i / a.G, h = g * a.G + i % a.G;
+    if (a.ml == nullptr) {
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      T* op = static_cast<T*>(a.out) + t * a.out_stride + h * HD + c0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) op[e] = from_f32<T>(v[e] * inv);
+      if (c0 == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(h) * a.T + t] = l == 0.f ? -INFINITY : m + logf(l);
+    } else {
+      const int64_t at = (static_cast<int64_t>(split) * a.T + t) * a.H + h;
+      if (c0 == 0) a.ml[at] = make_float2(m, l);
+      if (l != 0.f) *reinterpret_cast<float4*>(a.o + at * HD + c0) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+  }
+}
+
+// The parts of every row, joined: M = max m, L = sum l exp(m - M), out = sum o
+// exp(m - M) / L, in the splits' order. A part without keys has l = 0 and no o.
+// A thread takes four channels.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restrict__ ml,
+                                                         const float* __restrict__ o, int parts, int rows,
+                                                         int H, int Trows, T* __restrict__ out,
+                                                         int64_t out_stride, float* __restrict__ lse) {
+  constexpr int LPR = HD / 4;  // threads a row
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * (256 / LPR) + threadIdx.x / LPR;
+  const int c = (threadIdx.x % LPR) * 4;
+  if (i >= rows) return;
+  float M = -INFINITY;
+  for (int s = 0; s < parts; ++s) M = fmaxf(M, ml[static_cast<int64_t>(s) * rows + i].x);
+  const float m0 = M == -INFINITY ? 0.f : M;
+  float L = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < parts; ++s) {
+    const int64_t at = static_cast<int64_t>(s) * rows + i;
+    const float2 p = ml[at];
+    if (p.y == 0.f) continue;
+    const float f = expf(p.x - m0);
+    const float4 w = *reinterpret_cast<const float4*>(o + at * HD + c);
+    L = fmaf(p.y, f, L);
+    v[0] = fmaf(w.x, f, v[0]);
+    v[1] = fmaf(w.y, f, v[1]);
+    v[2] = fmaf(w.z, f, v[2]);
+    v[3] = fmaf(w.w, f, v[3]);
+  }
+  const int t = static_cast<int>(i / H), h = static_cast<int>(i - static_cast<int64_t>(t) * H);
+  const float inv = L == 0.f ? 0.f : 1.0f / L;
+  T* op = out + t * out_stride + h * HD + c;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) op[e] = from_f32<T>(v[e] * inv);
+  if (c == 0 && lse != nullptr) lse[static_cast<int64_t>(h) * Trows + t] = L == 0.f ? -INFINITY : M + logf(L);
+}
+
+template <typename T>
+hipError_t f32_dispatch(hipStream_t s, const PagedAttention& a, int64_t grid, int tiles, int splits) {
+  const dim3 g(static_cast<uint32_t>(grid)), block(256);
+  switch (a.hd) {
+    case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16>, g, block, 0, s, a, tiles, splits);
+    case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32>, g, block, 0, s, a, tiles, splits);
+    case 64: return launch(K_ATTENTION, paged_f32_kernel<T, 64>, g, block, 0, s, a, tiles, splits);
+    case 128: return launch(K_ATTENTION, paged_f32_kernel<T, 128>, g, block, 0, s, a, tiles, splits);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+template <typename T>
+hipError_t join_dispatch(hipStream_t s, const float2* ml, const float* o, int parts, int rows, int H, int T_,
+                         int hd, void* out, int64_t os, float* lse) {
+  const int per = 256 / (hd / 4);
+  const dim3 g(static_cast<uint32_t>((rows + per - 1) / per)), block(256);
+  T* op = static_cast<T*>(out);
+  switch (hd) {
+    case 16: return launch(K_ATTENTION, paged_join_kernel<T, 16>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse);
+    case 32: return launch(K_ATTENTION, paged_join_kernel<T, 32>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse);
+    case 64: return launch(K_ATTENTION, paged_join_kernel<T, 64>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse);
+    case 128: return launch(K_ATTENTION, paged_join_kernel<T, 128>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a) {
+  if (a.T == 0) return hipSuccess;
+  // few rows: one a workgroup, so that they spread over the CUs
+  const int rows = std::max(1, std::min(kAppendRows, a.T / (4 * device_cu_count())));
+  const dim3 grid((a.T + rows - 1) / rows), block(256);
+  if (dtype == 1) return launch(K_MISC, paged_append_kernel<bf16_t>, grid, block, 0, s, a, rows);
+  return launch(K_MISC, paged_append_kernel<float>, grid, block, 0, s, a, rows);
+}
+
+// Splits of the keys: enough workgroups for four a CU, none of fewer than 128 keys.
+int paged_chunk(int max_len, int64_t workgroups, int* splits) {
+  const int blocks = std::max(1, (max_len + 127) / 128);
+  const int64_t want = std::max<int64_t>(1, 4 * static_cast<int64_t>(device_cu_count()) / std::max<int64_t>(workgroups, 1));
+  const int per = static_cast<int>((blocks + std::min<int64_t>(want, blocks) - 1) / std::min<int64_t>(want, blocks));
+  *splits = (blocks + per - 1) / per;
+  return per * 128;
+}
+
+hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention& a, int max_rows, int splits) {
+  const int tiles = (max_rows + 31) / 32;
+  const int64_t grid = static_cast<int64_t>(splits) * tiles * (a.H / a.G) * a.B;
+  if (dtype == 1) return f32_dispatch<bf16_t>(s, a, grid, tiles, splits);
+  return f32_dispatch<float>(s, a, grid, tiles, splits);
+}
+
+hipError_t launch_paged_join(hipStream_t s, int dtype, const float2* ml, const float* o, int parts, int T, int H,
+                             int hd, void* out, int64_t out_stride, float* lse) {
+  if (dtype == 1) return join_dispatch<bf16_t>(s, ml, o, parts, T * H, H, T, hd, out, out_stride, lse);
+  return join_dispatch<float>(s, ml, o, parts, T * H, H, T, hd, out, out_stride, lse);
+}
+
+}  // namespace zsa

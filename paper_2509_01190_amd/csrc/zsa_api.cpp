@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "../../include/zsa.h"
+#include "zsa_check.h"
 #include "zsa_internal.h"
 
 namespace {
@@ -45,9 +46,15 @@ int hip_fail(hipError_t e, const char* what) {
     if (rc_ != ZSA_OK) return rc_; \
   } while (0)
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline size_t esize(int dtype) { return dtype == ZSA_BF16 ? 2 : 4; }
-inline size_t round256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
+using zsa::aligned16;
+using zsa::check_dtype;
+using zsa::check_head_dim;
+using zsa::check_kv_heads;
+using zsa::check_ptr16;
+using zsa::check_seqs;
+using zsa::check_width;
+using zsa::esize;
+using zsa::round256;
 
 // Eq. 2 for one sequence. The product and the sum are two separately
 // rounded IEEE double operations (the volatile store keeps the compiler from
@@ -68,44 +75,6 @@ int check_rate(double a) {
   return ZSA_OK;
 }
 
-// validate packed sequence offsets; returns total rows and the longest length
-int check_seqs(int32_t batch, const int32_t* cu_host, const int32_t* cu_dev, int32_t* total,
-               int32_t* max_len) {
-  if (batch < 0) return fail(ZSA_EINVAL, "batch %d < 0", batch);
-  if (cu_host == nullptr || cu_dev == nullptr) return fail(ZSA_EINVAL, "cu_host / cu_dev is NULL");
-  if (cu_host[0] != 0) return fail(ZSA_ESHAPE, "cu[0] = %d, must be 0", cu_host[0]);
-  int32_t ml = 0;
-  for (int b = 0; b < batch; ++b) {
-    const int32_t len = cu_host[b + 1] - cu_host[b];
-    if (len < 0) return fail(ZSA_ESHAPE, "cu not monotone at sequence %d", b);
-    if (len > ml) ml = len;
-  }
-  *total = cu_host[batch];
-  *max_len = ml;
-  return ZSA_OK;
-}
-
-int check_dtype(int32_t dtype) {
-  if (dtype != ZSA_F32 && dtype != ZSA_BF16) return fail(ZSA_EINVAL, "dtype %d unknown", dtype);
-  return ZSA_OK;
-}
-
-int check_ptr16(const void* p, const char* name, bool may_be_null = false) {
-  if (p == nullptr) {
-    if (may_be_null) return ZSA_OK;
-    return fail(ZSA_EINVAL, "%s is NULL", name);
-  }
-  if (!aligned16(p)) return fail(ZSA_EALIGN, "%s is not 16-byte aligned", name);
-  return ZSA_OK;
-}
-
-int check_width(int32_t dtype, int64_t width, const char* name) {
-  if (width <= 0) return fail(ZSA_ESHAPE, "%s = %lld must be positive", name, (long long)width);
-  if ((width * static_cast<int64_t>(esize(dtype))) % 16 != 0)
-    return fail(ZSA_EALIGN, "%s = %lld rows are not a multiple of 16 bytes", name, (long long)width);
-  return ZSA_OK;
-}
-
 // The bf16 attention kernels address one sequence's K/V rows (and the decode
 // kernel one cache slot's rows) through a buffer resource whose byte range
 // and per-tile offsets are 32-bit: the rows a kernel can reach must span
@@ -115,12 +84,6 @@ int check_row_range(int64_t rows, int64_t row_elems, int dtype, const char* what
     return fail(ZSA_EUNSUPPORTED,
                 "%s: %lld rows of %lld elements span 4 GiB or more (32-bit buffer offsets)", what,
                 (long long)rows, (long long)row_elems);
-  return ZSA_OK;
-}
-
-int check_head_dim(int32_t hd) {
-  if (hd != 16 && hd != 32 && hd != 64 && hd != 128)
-    return fail(ZSA_EUNSUPPORTED, "head_dim %d (supported: 16, 32, 64, 128)", hd);
   return ZSA_OK;
 }
 
@@ -538,15 +501,6 @@ size_t zsa_attention_workspace_size(int32_t n_heads, int32_t total_rows, int32_t
   size_t b = round256(static_cast<size_t>(n_heads) * total_rows * 4);  // lse scratch
   if (want_scores) b += round256(static_cast<size_t>(n_heads) * total_rows * 4);  // partials
   return b;
-}
-
-int check_kv_heads(int32_t n_heads, int32_t n_kv_heads, int* group) {
-  if (n_heads <= 0) return fail(ZSA_EINVAL, "n_heads %d", n_heads);
-  const int32_t hkv = n_kv_heads == 0 ? n_heads : n_kv_heads;
-  if (hkv < 0 || n_heads % hkv != 0)
-    return fail(ZSA_ESHAPE, "n_kv_heads %d must divide n_heads %d", n_kv_heads, n_heads);
-  *group = n_heads / hkv;
-  return ZSA_OK;
 }
 
 int zsa_attention_with_scores(void* stream, int32_t dtype, const void* q, const void* k,

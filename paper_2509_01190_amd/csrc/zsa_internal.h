@@ -424,6 +424,56 @@ hipError_t launch_decode_attention(hipStream_t s, const void* qkv, int64_t q_str
 int decode_splits_bound(int cap);
 bool decode_supported(int dtype, int hd, int group);
 
+// the key/value cache in pages (k_paged.hip). Strides in elements.
+struct PagedRows {            // where a sequence's cached rows lie
+  void* pool;                 // pages of 1 << shift rows [k | v], dtype
+  int64_t page_stride;
+  int shift, n_pages;
+  const int32_t* table;       // [batch][table_stride] page ids
+  int64_t table_stride;
+  int max_pages;              // ids a row of the table holds
+  int kvd;                    // key (and value) columns
+};
+struct PagedAppend {
+  PagedRows at;
+  const void *q, *k, *v;      // q null: none
+  int64_t q_stride, k_stride, v_stride;
+  void* q_out;
+  int64_t q_out_stride;
+  int H, Hkv, hd, T, B;
+  const int32_t* pos;         // null: rows are stored as they are
+  const int32_t *cu, *kv_len;
+  double inv_freq[kMaxHalfHead];
+};
+hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a);
+
+// One launch's attention over the rows of `at`. The query rows of a sequence
+// that read one key/value head are taken together: packed row i of head g is
+// new row i / G, query head g G + i % G.
+struct PagedAttention {
+  PagedRows at;
+  const void* q;
+  int64_t q_stride;
+  const int32_t* cu;          // null: all T rows are one sequence's (a common prefix)
+  const int32_t* kv_len;      // null: max_len rows
+  int max_len;                // rows from this one on are not read
+  int T, B, H, G, hd;
+  int causal;
+  float scale;
+  int chunk;                  // keys a split takes, a multiple of 128
+  void* out;                  // finished rows, when one split covers everything (ml null)
+  int64_t out_stride;
+  float* lse;                 // [H][T] or null
+  float2* ml;                 // [split][T * H] maximum and sum of the scores, else
+  float* o;                   // [split][T * H][hd] sums of values
+};
+// keys a split of up to max_len rows takes, and how many splits that makes
+int paged_chunk(int max_len, int64_t workgroups, int* splits);
+// max_rows: packed rows of the longest sequence
+hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention& a, int max_rows, int splits);
+hipError_t launch_paged_join(hipStream_t s, int dtype, const float2* ml, const float* o, int parts, int T, int H,
+                             int hd, void* out, int64_t out_stride, float* lse);
+
 // backward pass (bf16, head_dim 64 / 128 for the attention part)
 bool backward_supported(int dtype, int hd);
 // dW [m, n] = dY^T X over `rows` rows and db [m] = the column sums of dY (db

@@ -1,0 +1,265 @@
+// C entry points of the paged key/value cache: argument checks, the split of
+// the keys over workgroups and the workspace for the parts. As in
+// zsa_api.cpp, everything only enqueues work on the caller's stream.
+#include <algorithm>
+#include <math.h>
+
+#include "../../include/zsa.h"
+#include "zsa_check.h"
+#include "zsa_internal.h"
+
+namespace {
+
+using zsa::check_dtype;
+using zsa::check_head_dim;
+using zsa::check_kv_heads;
+using zsa::check_ptr16;
+using zsa::check_seqs;
+using zsa::check_width;
+using zsa::esize;
+using zsa::round256;
+using zsa::set_error;
+
+#define CHECK(expr)                \
+  do {                             \
+    const int rc_ = (expr);        \
+    if (rc_ != ZSA_OK) return rc_; \
+  } while (0)
+
+#define HIP_TRY(expr, what)                                                                    \
+  do {                                                                                         \
+    const hipError_t e_ = (expr);                                                              \
+    if (e_ != hipSuccess) return set_error(ZSA_EHIP, "%s: %s", what, hipGetErrorString(e_)); \
+  } while (0)
+
+// the cache's description; `rows`: the call has rows that use the table
+int check_cache(const zsa_paged_kv* c, bool rows) {
+  if (c == nullptr) return set_error(ZSA_EINVAL, "kv is NULL");
+  CHECK(check_dtype(c->dtype));
+  CHECK(check_head_dim(c->head_dim));
+  if (c->n_kv_heads <= 0) return set_error(ZSA_EINVAL, "n_kv_heads %d", c->n_kv_heads);
+  if (c->page_size < 16 || c->page_size > (1 << 20) || (c->page_size & (c->page_size - 1)) != 0)
+    return set_error(ZSA_EUNSUPPORTED, "page_size %d (a power of two from 16 to 2^20)", c->page_size);
+  if (c->n_pages < 0 || c->max_pages < 0)
+    return set_error(ZSA_ESHAPE, "n_pages %d, max_pages %d", c->n_pages, c->max_pages);
+  CHECK(check_ptr16(c->pool, "pool", !rows || c->n_pages == 0));
+  if (rows && c->table == nullptr && c->max_pages > 0) return set_error(ZSA_EINVAL, "table is NULL");
+  if (c->table_stride < c->max_pages)
+    return set_error(ZSA_ESHAPE, "table_stride %lld < max_pages %d", (long long)c->table_stride, c->max_pages);
+  CHECK(check_width(c->dtype, c->page_stride, "page_stride"));
+  const int64_t row = 2 * static_cast<int64_t>(c->n_kv_heads) * c->head_dim;
+  if (row > (1 << 20)) return set_error(ZSA_EUNSUPPORTED, "%d key/value heads of %d", c->n_kv_heads, c->head_dim);
+  if (c->page_stride < row * c->page_size)
+    return set_error(ZSA_ESHAPE, "page_stride %lld shorter than a page of %d rows of %lld",
+                     (long long)c->page_stride, c->page_size, (long long)row);
+  // the kernels reach a page's rows through 32-bit byte offsets
+  if (row * c->page_size * static_cast<int64_t>(esize(c->dtype)) >= (int64_t{1} << 31))
+    return set_error(ZSA_EUNSUPPORTED, "pages of 2 GiB or more");
+  return ZSA_OK;
+}
+
+zsa::PagedRows rows_of(const zsa_paged_kv& c) {
+  zsa::PagedRows r{};
+  r.pool = c.pool;
+  r.page_stride = c.page_stride;
+  r.shift = __builtin_ctz(static_cast<unsigned>(c.page_size));
+  r.n_pages = c.n_pages;
+  r.table = c.table;
+  r.table_stride = c.table_stride;
+  r.max_pages = c.max_pages;
+  r.kvd = c.n_kv_heads * c.head_dim;
+  return r;
+}
+
+int check_stride(int32_t dtype, int64_t stride, int64_t width, const char* name) {
+  CHECK(check_width(dtype, stride, name));
+  if (stride < width) return set_error(ZSA_ESHAPE, "%s %lld < %lld columns", name, (long long)stride, (long long)width);
+  return ZSA_OK;
+}
+
+size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
+  return round256(parts * rows * sizeof(float2)) + round256(parts * rows * hd * sizeof(float));
+}
+
+// The splits of a call's own rows and of the common prefix (0: none).
+struct Plan {
+  int chunk, splits;    // of the sequences' own rows
+  int pchunk, psplits;  // of the prefix
+  int parts() const { return psplits + splits; }
+  bool direct() const { return parts() == 1; }
+};
+
+Plan plan_of(int dtype, int hd, int H, int Hkv, int batch, int max_new, int T, int max_len, int prefix) {
+  Plan p{};
+  const int G = H / Hkv;
+  const int64_t rows = std::min<int64_t>(static_cast<int64_t>(max_new) * G, 1 << 30);
+  p.chunk = zsa::paged_chunk(max_len, (rows + 31) / 32 * Hkv * batch, &p.splits);
+  if (prefix > 0)
+    p.pchunk = zsa::paged_chunk(prefix, (static_cast<int64_t>(T) * G + 31) / 32 * Hkv, &p.psplits);
+  return p;
+}
+
+int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_heads,
+              int32_t causal, float scale, int32_t batch, const int32_t* cu_host, const int32_t* cu_dev,
+              const int32_t* kv_len, int32_t max_kv_len, const int32_t* prefix_pages, int32_t prefix_len,
+              void* out, int64_t out_stride, float* lse, void* ws, size_t ws_bytes) {
+  int32_t T, max_new;
+  CHECK(check_seqs(batch, cu_host, cu_dev, &T, &max_new));
+  CHECK(check_cache(kv, T > 0));
+  int G = 1;
+  if (n_heads <= 0) return set_error(ZSA_EINVAL, "n_heads %d", n_heads);
+  CHECK(check_kv_heads(n_heads, kv->n_kv_heads, &G));
+  if (!(scale > 0.f)) return set_error(ZSA_EINVAL, "scale must be positive");
+  if (max_kv_len < 0 || prefix_len < 0)
+    return set_error(ZSA_EINVAL, "max_kv_len %d, prefix_len %d", max_kv_len, prefix_len);
+  const int64_t width = static_cast<int64_t>(n_heads) * kv->head_dim;
+  CHECK(check_stride(kv->dtype, q_stride, width, "q_stride"));
+  CHECK(check_stride(kv->dtype, out_stride, width, "out_stride"));
+  CHECK(check_ptr16(q, "q", T == 0));
+  CHECK(check_ptr16(out, "out", T == 0));
+  if (T > 0 && kv_len == nullptr) return set_error(ZSA_EINVAL, "kv_len is NULL");
+  if (T > 0 && prefix_len > 0 && prefix_pages == nullptr) return set_error(ZSA_EINVAL, "prefix_pages is NULL");
+  if (max_kv_len > static_cast<int64_t>(kv->max_pages) * kv->page_size)
+    return set_error(ZSA_ESHAPE, "max_kv_len %d beyond the table's %d pages of %d rows", max_kv_len, kv->max_pages,
+                     kv->page_size);
+  if (static_cast<int64_t>(T) * n_heads >= (int64_t{1} << 31))
+    return set_error(ZSA_EUNSUPPORTED, "%d rows of %d heads: 2^31 or more", T, n_heads);
+  const size_t need = zsa_paged_attention_workspace_size(kv, n_heads, batch, cu_host, max_kv_len, prefix_len);
+  if (need > 0) {
+    CHECK(check_ptr16(ws, "ws"));
+    if (ws_bytes < need) return set_error(ZSA_EWORKSPACE, "workspace %zu bytes < %zu", ws_bytes, need);
+  }
+  if (T == 0) return ZSA_OK;
+  const Plan p = plan_of(kv->dtype, kv->head_dim, n_heads, kv->n_kv_heads, batch, max_new, T, max_kv_len, prefix_len);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int64_t rows = static_cast<int64_t>(T) * n_heads;
+  float2* ml = p.direct() ? nullptr : static_cast<float2*>(ws);
+  float* o = p.direct() ? nullptr
+                        : reinterpret_cast<float*>(static_cast<char*>(ws) + round256(p.parts() * rows * sizeof(float2)));
+  zsa::PagedAttention a{};
+  a.at = rows_of(*kv);
+  a.q = q;
+  a.q_stride = q_stride;
+  a.cu = cu_dev;
+  a.kv_len = kv_len;
+  a.max_len = max_kv_len;
+  a.T = T;
+  a.B = batch;
+  a.H = n_heads;
+  a.G = G;
+  a.hd = kv->head_dim;
+  a.causal = causal != 0;
+  a.scale = scale;
+  a.chunk = p.chunk;
+  a.out = out;
+  a.out_stride = out_stride;
+  a.lse = lse;
+  a.ml = ml;
+  a.o = o;
+  if (p.psplits > 0) {
+    zsa::PagedAttention f = a;
+    f.at.table = prefix_pages;
+    f.at.max_pages = static_cast<int>((static_cast<int64_t>(prefix_len) + kv->page_size - 1) / kv->page_size);
+    f.cu = nullptr;
+    f.kv_len = nullptr;
+    f.max_len = prefix_len;
+    f.B = 1;
+    f.causal = 0;
+    f.chunk = p.pchunk;
+    HIP_TRY(zsa::launch_paged_attention(s, kv->dtype, f, T * G, p.psplits), "prefix attention");
+    a.ml = ml + p.psplits * rows;
+    a.o = o + p.psplits * rows * kv->head_dim;
+  }
+  HIP_TRY(zsa::launch_paged_attention(s, kv->dtype, a, max_new * G, p.splits), "paged attention");
+  if (ml != nullptr)
+    HIP_TRY(zsa::launch_paged_join(s, kv->dtype, ml, o, p.parts(), T, n_heads, kv->head_dim, out, out_stride, lse),
+            "paged attention's parts");
+  return ZSA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int zsa_paged_append(void* stream, const zsa_paged_kv* kv, const void* k, int64_t k_stride, const void* v,
+                     int64_t v_stride, const void* q, int64_t q_stride, int32_t n_heads, void* q_out,
+                     int64_t q_out_stride, const int32_t* pos, float rope_theta, int32_t batch,
+                     const int32_t* cu_host, const int32_t* cu_dev, const int32_t* kv_len) {
+  int32_t T, max_new;
+  CHECK(check_seqs(batch, cu_host, cu_dev, &T, &max_new));
+  CHECK(check_cache(kv, T > 0));
+  const int64_t kvd = static_cast<int64_t>(kv->n_kv_heads) * kv->head_dim;
+  CHECK(check_ptr16(k, "k", T == 0));
+  CHECK(check_ptr16(v, "v", T == 0));
+  CHECK(check_stride(kv->dtype, k_stride, kvd, "k_stride"));
+  CHECK(check_stride(kv->dtype, v_stride, kvd, "v_stride"));
+  if (q != nullptr) {
+    int G = 1;
+    if (n_heads <= 0) return set_error(ZSA_EINVAL, "n_heads %d", n_heads);
+    CHECK(check_kv_heads(n_heads, kv->n_kv_heads, &G));
+    if (pos == nullptr) return set_error(ZSA_EINVAL, "q without pos: nothing would rotate it");
+    CHECK(check_ptr16(q, "q"));
+    CHECK(check_ptr16(q_out, "q_out"));
+    const int64_t width = static_cast<int64_t>(n_heads) * kv->head_dim;
+    CHECK(check_stride(kv->dtype, q_stride, width, "q_stride"));
+    CHECK(check_stride(kv->dtype, q_out_stride, width, "q_out_stride"));
+  }
+  if (pos != nullptr && !(rope_theta > 0.f)) return set_error(ZSA_EINVAL, "rope_theta <= 0");
+  if (T > 0 && kv_len == nullptr) return set_error(ZSA_EINVAL, "kv_len is NULL");
+  if (T == 0) return ZSA_OK;
+  zsa::PagedAppend a{};
+  a.at = rows_of(*kv);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out = q_out;
+  a.q_out_stride = q_out_stride;
+  a.H = n_heads;
+  a.Hkv = kv->n_kv_heads;
+  a.hd = kv->head_dim;
+  a.T = T;
+  a.B = batch;
+  a.pos = pos;
+  a.cu = cu_dev;
+  a.kv_len = kv_len;
+  if (pos != nullptr)
+    for (int i = 0; i < kv->head_dim / 2; ++i)
+      a.inv_freq[i] = pow(static_cast<double>(rope_theta), -2.0 * i / kv->head_dim);
+  HIP_TRY(zsa::launch_paged_append(static_cast<hipStream_t>(stream), kv->dtype, a), "paged append");
+  return ZSA_OK;
+}
+
+size_t zsa_paged_attention_workspace_size(const zsa_paged_kv* kv, int32_t n_heads, int32_t batch,
+                                          const int32_t* cu_host, int32_t max_kv_len, int32_t prefix_len) {
+  if (kv == nullptr || cu_host == nullptr || batch <= 0 || n_heads <= 0 || kv->n_kv_heads <= 0 ||
+      n_heads % kv->n_kv_heads != 0 || max_kv_len < 0 || prefix_len < 0)
+    return 0;
+  int max_new = 0;
+  for (int b = 0; b < batch; ++b) max_new = std::max(max_new, cu_host[b + 1] - cu_host[b]);
+  const int T = cu_host[batch];
+  if (T <= 0) return 0;
+  const Plan p = plan_of(kv->dtype, kv->head_dim, n_heads, kv->n_kv_heads, batch, max_new, T, max_kv_len, prefix_len);
+  return p.direct() ? 0 : parts_bytes(p.parts(), static_cast<int64_t>(T) * n_heads, kv->head_dim);
+}
+
+int zsa_paged_attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_heads,
+                        int32_t causal, float scale, int32_t batch, const int32_t* cu_host,
+                        const int32_t* cu_dev, const int32_t* kv_len, int32_t max_kv_len, void* out,
+                        int64_t out_stride, float* lse, void* ws, size_t ws_bytes) {
+  return attention(stream, kv, q, q_stride, n_heads, causal, scale, batch, cu_host, cu_dev, kv_len, max_kv_len,
+                   nullptr, 0, out, out_stride, lse, ws, ws_bytes);
+}
+
+int zsa_prefix_attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_heads,
+                         int32_t causal, float scale, int32_t batch, const int32_t* cu_host,
+                         const int32_t* cu_dev, const int32_t* kv_len, int32_t max_kv_len,
+                         const int32_t* prefix_pages, int32_t prefix_len, void* out, int64_t out_stride,
+                         float* lse, void* ws, size_t ws_bytes) {
+  return attention(stream, kv, q, q_stride, n_heads, causal, scale, batch, cu_host, cu_dev, kv_len, max_kv_len,
+                   prefix_pages, prefix_len, out, out_stride, lse, ws, ws_bytes);
+}
+
+}  // extern "C"

@@ -61,6 +61,13 @@ class LayerGrads(ctypes.Structure):
     _fields_ = [(n, _vp) for n in WEIGHT_NAMES]
 
 
+class PagedKvStruct(ctypes.Structure):
+    _fields_ = [("pool", _vp), ("table", _vp), ("page_stride", _i64), ("table_stride", _i64),
+                ("n_pages", _i32), ("page_size", _i32), ("max_pages", _i32), ("n_kv_heads", _i32),
+                ("head_dim", _i32), ("dtype", _i32)]
+
+
+_PKV = ctypes.POINTER(PagedKvStruct)
 _SIGS = {
     "zsa_last_error": (ctypes.c_char_p, []),
     "zsa_version": (ctypes.c_char_p, []),
@@ -101,6 +108,13 @@ _SIGS = {
                                           _vp, _vp, _vp, _sz]),
     "zsa_stack_backward_workspace_size": (_sz, [ctypes.POINTER(LayerCfg), _i32, _i32, _i32, _i32]),
     "zsa_stack_workspace_size": (_sz, [ctypes.POINTER(LayerCfg), _i32, _i32, _i32]),
+    "zsa_paged_append": (ctypes.c_int, [_vp, _PKV, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _i64,
+                                        _vp, _f32, _i32, _pi32, _vp, _vp]),
+    "zsa_paged_attention": (ctypes.c_int, [_vp, _PKV, _vp, _i64, _i32, _i32, _f32, _i32, _pi32, _vp,
+                                           _vp, _i32, _vp, _i64, _vp, _vp, _sz]),
+    "zsa_prefix_attention": (ctypes.c_int, [_vp, _PKV, _vp, _i64, _i32, _i32, _f32, _i32, _pi32, _vp,
+                                            _vp, _i32, _vp, _i32, _vp, _i64, _vp, _vp, _sz]),
+    "zsa_paged_attention_workspace_size": (_sz, [_PKV, _i32, _i32, _pi32, _i32, _i32]),
     "zsa_timing_arm": (ctypes.c_int, [_i32, _i32]),
     "zsa_timing_read": (ctypes.c_int, [_i32, _pi32, ctypes.POINTER(ctypes.c_double)]),
 }
@@ -193,6 +207,15 @@ class Seqs:
         self.batch = len(host) - 1
         self.total = int(host[-1])
         return self
+
+    @classmethod
+    def wrap(cls, cu, cu_dev: torch.Tensor) -> "Seqs":
+        """Offsets that the caller holds on both sides already: ``cu`` on the
+        host, ``cu_dev`` the same int32 values on the device."""
+        host = _host_i32(cu)
+        if cu_dev.dtype != torch.int32 or not cu_dev.is_contiguous() or cu_dev.numel() != len(host):
+            raise ValueError("cu_dev must hold the host's offsets as contiguous int32")
+        return cls._of(host, cu_dev)
 
     @property
     def lengths(self) -> List[int]:
@@ -334,6 +357,138 @@ def compact_gather(hidden: torch.Tensor, pos: Optional[torch.Tensor],
     _check(lib().zsa_compact_gather(_stream(hidden.device), _dtype_code(hidden), _p(hidden), d,
                                     _p(pos), t_in, _p(kept_rows), t_out, _p(out), _p(pos_out)))
     return out, pos_out
+
+
+# ------------------------------------------------------------------ paged cache
+class PagedKV:
+    """One layer's key/value cache in pages (include/zsa.h, zsa_paged_kv).
+
+    ``pool`` [pages, page_size, 2 * n_kv_heads * hd] on the device (a page's
+    rows contiguous; the pages may lie apart, as in pool[:, layer] of one
+    tensor for all layers), ``table`` [batch, pages a sequence] int32 on the
+    same device. Both stay the caller's."""
+
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, n_kv_heads: int):
+        _require_cuda(pool, table)
+        if pool.dim() != 3 or table.dim() != 2 or table.dtype != torch.int32:
+            raise ValueError("pool must be [pages, page_size, 2 * kvd] and table [batch, pages] int32")
+        pages, size, width = pool.shape
+        if n_kv_heads < 1 or width % (2 * n_kv_heads) != 0:
+            raise ValueError(f"rows of {width} are not keys and values of {n_kv_heads} heads")
+        if pages > 0 and (pool.stride(2) != 1 or pool.stride(1) != width):
+            raise ValueError("a page's rows must be contiguous")
+        if table.numel() > 0 and table.shape[1] > 1 and table.stride(1) != 1:
+            raise ValueError("a sequence's page ids must be contiguous")
+        if table.device != pool.device:
+            raise ValueError("pool and table must be on one device")
+        self.pool, self.table, self.n_kv_heads = pool, table, n_kv_heads
+        self.head_dim = width // (2 * n_kv_heads)
+        batch, most = table.shape
+        self._struct = PagedKvStruct(
+            pool.data_ptr() or None, table.data_ptr() or None,
+            pool.stride(0) if pages > 1 else size * width, table.stride(0) if batch > 1 else most,
+            pages, size, most, n_kv_heads, self.head_dim, _dtype_code(pool))
+        self._ref = ctypes.byref(self._struct)
+
+
+def _paged_rows(kv: PagedKV, seqs: Seqs, kv_len: torch.Tensor, rows: torch.Tensor, what: str) -> int:
+    """Checks a call's rows against the cache; returns their stride."""
+    _require_cuda(rows, kv_len, seqs.dev)
+    if seqs.batch != kv.table.shape[0]:
+        raise ValueError(f"{seqs.batch} sequences, {kv.table.shape[0]} rows of the table")
+    if kv_len.dtype != torch.int32 or kv_len.numel() != seqs.batch or not kv_len.is_contiguous():
+        raise ValueError("kv_len must be contiguous int32, one a sequence")
+    return _rows_stride(kv, seqs, rows, what)
+
+
+def _rows_stride(kv: PagedKV, seqs: Seqs, rows: torch.Tensor, what: str) -> int:
+    if rows.dim() != 2 or rows.shape[0] != seqs.total:
+        raise ValueError(f"{what} must have {seqs.total} rows")
+    if rows.dtype != kv.pool.dtype or rows.device != kv.pool.device:
+        raise ValueError(f"{what} must have the cache's type and device")
+    if rows.numel() > 0 and rows.stride(1) != 1:
+        raise ValueError(f"{what}'s columns must be contiguous")
+    return rows.stride(0) if rows.shape[0] > 1 else rows.shape[1]
+
+
+def paged_append(kv: PagedKV, k: torch.Tensor, v: torch.Tensor, seqs: Seqs, kv_len: torch.Tensor,
+                 pos: Optional[torch.Tensor] = None, rope_theta: float = 10000.0,
+                 q: Optional[torch.Tensor] = None, n_heads: int = 0) -> Optional[torch.Tensor]:
+    """Appends the new rows k, v [T, n_kv_heads * hd] (views with any row
+    stride) to the cache: kv_len [batch] int32 on the device counts each
+    sequence's rows with the new ones, which are the last. With ``pos`` [T]
+    int32 the keys are rotated on the way, and so are the queries ``q``
+    [T, n_heads * hd] if given, which are returned."""
+    ks = _paged_rows(kv, seqs, kv_len, k, "k")
+    vs = _rows_stride(kv, seqs, v, "v")
+    kvd = kv.n_kv_heads * kv.head_dim
+    if k.shape[1] != kvd or v.shape[1] != kvd:
+        raise ValueError(f"k and v must have {kvd} columns")
+    if pos is not None:
+        _require_cuda(pos)
+        if pos.dtype != torch.int32 or pos.numel() != seqs.total or not pos.is_contiguous():
+            raise ValueError("pos must be contiguous int32, one a row")
+    out, qs, qos = None, 0, 0
+    if q is not None:
+        qs = _rows_stride(kv, seqs, q, "q")
+        if n_heads < 1 or q.shape[1] != n_heads * kv.head_dim:
+            raise ValueError(f"q must have {n_heads} heads of {kv.head_dim}")
+        out = torch.empty((seqs.total, q.shape[1]), dtype=q.dtype, device=q.device)
+        qos = q.shape[1]
+    if seqs.total == 0:
+        return out
+    with torch.cuda.device(k.device):
+        _check(lib().zsa_paged_append(
+            _stream(k.device), kv._ref, _p(k), ks, _p(v), vs, _p(q), qs, n_heads, _p(out), qos, _p(pos),
+            rope_theta, seqs.batch, _hp32(seqs.host), _p(seqs.dev), _p(kv_len)))
+    return out
+
+
+def prefix_attention(q: torch.Tensor, kv: PagedKV, n_heads: int, seqs: Seqs, kv_len: torch.Tensor,
+                     prefix_pages: Optional[torch.Tensor], prefix_len: int,
+                     max_kv_len: Optional[int] = None, causal: bool = True, want_lse: bool = False,
+                     scale: Optional[float] = None):
+    """paged_attention for sequences that share their first ``prefix_len``
+    rows, which lie in the pages ``prefix_pages`` (int32, on the device)
+    and come before the rows that kv_len counts. Returns (out, lse or None)."""
+    qs = _paged_rows(kv, seqs, kv_len, q, "q")
+    hd, size = kv.head_dim, kv.pool.shape[1]
+    if q.shape[1] != n_heads * hd:
+        raise ValueError(f"q must have {n_heads} heads of {hd}")
+    if prefix_len > 0:
+        if prefix_pages is None:
+            raise ValueError("prefix_pages is missing")
+        _require_cuda(prefix_pages)
+        if (prefix_pages.dtype != torch.int32 or not prefix_pages.is_contiguous()
+                or prefix_pages.numel() * size < prefix_len or prefix_pages.device != q.device):
+            raise ValueError("prefix_pages must be contiguous int32 ids of pages that hold prefix_len rows")
+    if max_kv_len is None:
+        max_kv_len = kv.table.shape[1] * size
+    if scale is None:
+        scale = 1.0 / float(np.sqrt(hd))
+    T = seqs.total
+    out = torch.empty((T, n_heads * hd), dtype=q.dtype, device=q.device)
+    lse = torch.empty((n_heads, T), dtype=torch.float32, device=q.device) if want_lse else None
+    cu = _hp32(seqs.host)
+    with torch.cuda.device(q.device):
+        wsz = lib().zsa_paged_attention_workspace_size(kv._ref, n_heads, seqs.batch, cu, max_kv_len, prefix_len)
+        ws = torch.empty(wsz, dtype=torch.uint8, device=q.device) if wsz else None
+        _check(lib().zsa_prefix_attention(
+            _stream(q.device), kv._ref, _p(q), qs, n_heads, int(causal), scale, seqs.batch, cu,
+            _p(seqs.dev), _p(kv_len), max_kv_len, _p(prefix_pages), prefix_len, _p(out), n_heads * hd,
+            _p(lse), _p(ws), wsz))
+    return out, lse
+
+
+def paged_attention(q: torch.Tensor, kv: PagedKV, n_heads: int, seqs: Seqs, kv_len: torch.Tensor,
+                    max_kv_len: Optional[int] = None, causal: bool = True, want_lse: bool = False,
+                    scale: Optional[float] = None):
+    """Attention of the new rows q [T, n_heads * hd] over their sequences'
+    cached rows, the new ones (appended before) included. ``kv_len`` [batch]
+    int32 is read on the device; ``max_kv_len`` bounds it on the host (the
+    table's rows if not given). A row that sees no key gives 0 and lse -inf.
+    Returns (out, lse or None)."""
+    return prefix_attention(q, kv, n_heads, seqs, kv_len, None, 0, max_kv_len, causal, want_lse, scale)
 
 
 # ------------------------------------------------------------------ blocks
