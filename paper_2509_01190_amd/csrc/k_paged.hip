@@ -24,7 +24,11 @@
 namespace zsa {
 namespace {
 
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 
 // ---------------------------------------------------------------------------
 // append
@@ -133,6 +137,264 @@ __device__ __forceinline__ Span span_of(const PagedAttention& a, int b) {
   s.first = len - n + 1;
   s.table = a.at.table + (a.cu != nullptr ? b * a.at.table_stride : 0);
   return s;
+}
+
+// the page ids and lengths, read as scalars: loads that would wait in line
+// with a wave's tile loads otherwise
+typedef const __attribute__((address_space(4))) int32_t* scalar_ids;
+__device__ __forceinline__ scalar_ids scalar(const int32_t* p) {
+  return reinterpret_cast<scalar_ids>(reinterpret_cast<uintptr_t>(p));
+}
+
+// bf16, heads of 64 and 128, up to 32 packed rows at a time: bound by the
+// cached rows' bytes. A workgroup takes 32 packed rows of one (sequence,
+// key/value head) and a split of its keys; its four waves take 32-key tiles in
+// turn, each through its own K and V buffer in LDS, without barriers: the next
+// tile's K is under way as soon as S^T = K Q^T has read the last one, its V
+// after O^T += V^T P^T has. A load instruction covers whole rows of a head (4
+// of 128, 8 of 64) of one page, through a buffer resource that ends with the
+// sequence, so what lies behind its last row reads as zeros, and so does a
+// page outside the pool. The transposed products leave a lane the scores of
+// one row, which are the operand of the second product (k_attn.hip). P meets V
+// as two bf16 numbers whose sum has 16 bits: the matrix cores have the time.
+template <int HD>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2))) void paged_few_kernel(
+    PagedAttention a, int tiles, int splits) {
+  constexpr int NW = 4, KK = HD / 16, CT = HD / 32, CPR = HD / 8;
+  constexpr int RB = HD * 2, HALF = 32 * RB;    // a tile of 32 rows of K, or V
+  constexpr int RPL = 1024 / RB, NL = 16 / RPL;  // rows a load, loads per 16 rows
+  constexpr int HP = 33;                         // merge row stride: [channel][row]
+  constexpr int SBYTES = NW * HD * HP * 4 > NW * 2 * HALF ? NW * HD * HP * 4 : NW * 2 * HALF;
+  __shared__ __align__(1024) unsigned char smem[SBYTES];
+  __shared__ float sm[NW][32], sl[NW][32];
+  const int split = blockIdx.x % splits, it0 = blockIdx.x / splits;
+  const int tile = it0 % tiles, gb = it0 / tiles, Hkv = a.H / a.G, g = gb % Hkv, b = gb / Hkv;
+  const Span sp = span_of(a, b);
+  const int i0 = tile * 32;
+  if (i0 >= sp.rows) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, l32 = lane & 31;
+  const int row = min(i0 + l32, sp.rows - 1);  // rows past the sequence are not stored
+  const int lim = a.causal ? min(sp.first + row / a.G, sp.len) : sp.len;
+  const int lim0 = a.causal ? min(sp.first + i0 / a.G, sp.len) : sp.len;  // the tile's first row's
+  const int last = a.causal ? min(sp.first + min(i0 + 31, sp.rows - 1) / a.G, sp.len) : sp.len;
+  const int k0 = split * a.chunk, kend = min(last, k0 + a.chunk);
+  const float scale_log2 = a.scale * kLog2e;
+
+  // K row r of a tile keeps its 16-byte chunk c at c ^ ksw(r), V row r at c ^ vsw(r) (k_attn.hip)
+  auto ksw = [](int r) { return HD == 64 ? (r >> 1) & 7 : r & 15; };
+  auto vsw = [](int r) { return HD == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; };
+  const uint32_t rowb = static_cast<uint32_t>(a.at.kvd) * 4u;
+  uint32_t koff[NL], voff[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int r = i * RPL + lane / CPR;
+    koff[i] = r * rowb + (((lane % CPR) ^ ksw(r)) << 4);
+    voff[i] = r * rowb + (((lane % CPR) ^ vsw(r)) << 4);
+  }
+  unsigned char* mine = smem + wave * (2 * HALF);
+  const uint32_t lds0 = lds_address(smem) + wave * (2 * HALF);
+  const scalar_ids table = scalar(sp.table);
+  const char* pool = static_cast<const char*>(a.at.pool);
+  // 16 rows from row j on, of page `page` (-1 where the sequence has ended): `col` bytes into a row
+  auto resource = [&](int j, int page, uint32_t col) {
+    const bool there = page >= 0 && page < a.at.n_pages;
+    const uint32_t bytes = there ? static_cast<uint32_t>(min(sp.len - j, 16)) * rowb - col : 0u;
+    u32x4 res = buffer_resource(pool + (there ? page : 0) * (a.at.page_stride * 2) +
+                                    static_cast<uint32_t>(j & ((1 << a.at.shift) - 1)) * rowb + col,
+                                bytes);
+    // a load in asm may follow a vector instruction's write of its scalar operands by five states at least
+    asm volatile("s_nop 4" : "+s"(res));
+    return res;
+  };
+  auto page_of = [&](int j) { return j < sp.len ? table[j >> a.at.shift] : -1; };
+  const uint32_t kcol = g * RB, vcol = rowb / 2 + g * RB;
+  auto load = [&](int j0, int pg0, int pg1, uint32_t lds, uint32_t col, const uint32_t (&off)[NL]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 res = resource(j0 + 16 * h, h == 0 ? pg0 : pg1, col);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) lds_load16(lds + (h * NL + i) * 1024, off[i], res);
+    }
+  };
+
+  float m_run = -INFINITY, l_run = 0.f;  // of the raw scores; l_run: this lane's keys only
+  f32x16_t o[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
+  // fragment addresses (k_attn.hip)
+  const uint32_t vrow = 4 * half + ((lane & 15) >> 2);
+  const int ks0 = ksw(l32), vs0 = vsw(vrow);
+  const int vch = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+  const f32x16_t zero = {};
+
+  int j0 = k0 + wave * 32;
+  int pg0 = page_of(j0), pg1 = page_of(j0 + 16);
+  if (j0 < kend) {
+    load(j0, pg0, pg1, lds0, kcol, koff);
+    load(j0, pg0, pg1, lds0 + HALF, vcol, voff);
+  }
+  bf16x8_t qf[KK];
+  {
+    const bf16_t* qp = static_cast<const bf16_t*>(a.q) + static_cast<int64_t>(sp.lo + row / a.G) * a.q_stride +
+                       (g * a.G + row % a.G) * HD;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      qf[kk] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(qp + kk * 16 + half * 8));
+    // here before the loop, which would otherwise wait for every load in it
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]));
+  }
+  for (; j0 < kend; j0 += 32 * NW) {
+    const int jn = j0 + 32 * NW;
+    const bool more = jn < kend;
+    pg0 = page_of(jn);
+    pg1 = page_of(jn + 16);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // K is here, V may be under way
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16_t s;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const bf16x8_t k = __builtin_bit_cast(
+          bf16x8_t, *reinterpret_cast<const u32x4*>(mine + l32 * RB + (((2 * kk + half) ^ ks0) << 4)));
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[kk], kk == 0 ? zero : s, 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) load(jn, pg0, pg1, lds0, kcol, koff);
+    // s[r]: key j0 + 8 (r/4) + 4 half + r%4, packed row `row`
+    if (j0 + 32 > lim0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (j0 + 8 * (r >> 2) + 4 * half + (r & 3) >= lim) s[r] = -INFINITY;
+    }
+    float mloc = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mloc = fmaxf(mloc, s[r]);
+    mloc = half_swap_max(mloc);
+    // the reference maximum moves only when it has to (k_attn.hip)
+    const float m_new = fmaxf(m_run, mloc);
+    if (__builtin_amdgcn_ballot_w64(m_new == -INFINITY ? false : !((m_new - m_run) * scale_log2 <= 8.0f)) != 0) {
+      const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m_run - m_new) * scale_log2);
+      l_run *= alpha;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
+      m_run = m_new;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run * scale_log2;
+    u32x4 hi[2], lo[2];
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[r], scale_log2, -m_use));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(s[r + 1], scale_log2, -m_use));
+      l_run += p0 + p1;
+      s[r] = p0;
+      s[r + 1] = p1;
+      const uint32_t w = pack_bf16x2(p0, p1);
+      hi[r >> 3][(r >> 1) & 3] = w;
+      lo[r >> 3][(r >> 1) & 3] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u));
+    }
+    if (more)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // V is here, the next K may be under way
+    else
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    // A value that is not finite must not reach a row that does not see its
+    // key, through the product with its zero probability: where the tile holds
+    // hidden keys and such values, it goes through the vector ALU, key by key.
+    bool odd = false;
+    if (lim0 < min(j0 + 32, sp.len)) {
+#pragma unroll
+      for (int i = 0; i < 2 * NL; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(mine + HALF + i * 1024 + lane * 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          odd |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+      }
+      odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+    }
+    if (!odd) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const unsigned char* vr = mine + HALF + (16 * k + vrow) * RB + (lane & 1) * 8 + (((4 * ct + vch) ^ vs0) << 4);
+          const bf16x8_t v = __builtin_bit_cast(bf16x8_t, lds_read_columns(vr, vr + 8 * RB));
+          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, hi[k]), o[ct], 0, 0, 0);
+          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, lo[k]), o[ct], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < 32; ++kk) {
+        // key j0 + kk: register (kk / 8) * 4 + kk % 4 of lane half (kk / 4) % 2
+        const float p = __shfl(s[(kk >> 3) * 4 + (kk & 3)], l32 + 32 * ((kk >> 2) & 1), 64);
+        if (j0 + kk < lim) {
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+              const int c = ct * 32 + 2 * r + 4 * half;
+              const uint2 w = *reinterpret_cast<const uint2*>(mine + HALF + kk * RB + (((c >> 3) ^ vsw(kk)) << 4) + (c & 7) * 2);
+              o[ct][r] = fmaf(p, __uint_as_float(w.x << 16), o[ct][r]);
+              o[ct][r + 1] = fmaf(p, __uint_as_float(w.x & 0xffff0000u), o[ct][r + 1]);
+              o[ct][r + 2] = fmaf(p, __uint_as_float(w.y << 16), o[ct][r + 2]);
+              o[ct][r + 3] = fmaf(p, __uint_as_float(w.y & 0xffff0000u), o[ct][r + 3]);
+            }
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) load(jn, pg0, pg1, lds0 + HALF, vcol, voff);
+  }
+  l_run = half_swap_sum(l_run);
+  __syncthreads();  // every wave is past its tiles
+  float* so = reinterpret_cast<float*>(smem);
+  if (half == 0) {
+    sm[wave][l32] = m_run == -INFINITY ? -INFINITY : m_run * scale_log2;
+    sl[wave][l32] = l_run;
+  }
+  const int nr = min(32, sp.rows - i0);
+  if (l32 < nr) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        so[(wave * HD + ct * 32 + 8 * (r >> 2) + 4 * half + (r & 3)) * HP + l32] = o[ct][r];
+  }
+  __syncthreads();
+  for (int it = tid; it < nr * (HD / 4); it += 64 * NW) {
+    const int q = it / (HD / 4), c0 = (it % (HD / 4)) * 4, i = i0 + q;
+    float m = sm[0][q];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, sm[w][q]);
+    float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      // a wave without keys for this row holds the empty sum
+      if (sm[w][q] == -INFINITY && sl[w][q] == 0.f) continue;
+      const float f = __builtin_amdgcn_exp2f(sm[w][q] - (m == -INFINITY ? 0.f : m));
+      l = fmaf(f, sl[w][q], l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(f, so[(w * HD + c0 + e) * HP + q], v[e]);
+    }
+    const int t = sp.lo + i / a.G, h = g * a.G + i % a.G;
+    if (a.ml == nullptr) {
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + t * a.out_stride + h * HD + c0) =
+          make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
+      if (c0 == 0 && a.lse != nullptr)
+        a.lse[static_cast<int64_t>(h) * a.T + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    } else {
+      const int64_t at = (static_cast<int64_t>(split) * a.T + t) * a.H + h;
+      if (c0 == 0) a.ml[at] = make_float2(m, l);
+      if (l != 0.f) *reinterpret_cast<float4*>(a.o + at * HD + c0) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+  }
 }
 
 // fp32 storage, and bf16 at head dims 16 and 32: both products on
@@ -315,13 +577,15 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedAttention a, int ti
 
 // The parts of every row, joined: M = max m, L = sum l exp(m - M), out = sum o
 // exp(m - M) / L, in the splits' order. A part without keys has l = 0 and no o.
-// A thread takes four channels.
+// A thread takes four channels. (The bf16 matrix kernels' maxima are in units
+// of log 2, as they used them.)
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restrict__ ml,
                                                          const float* __restrict__ o, int parts, int rows,
                                                          int H, int Trows, T* __restrict__ out,
                                                          int64_t out_stride, float* __restrict__ lse) {
   constexpr int LPR = HD / 4;  // threads a row
+  constexpr bool LOG2 = sizeof(T) == 2 && HD >= 64;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * (256 / LPR) + threadIdx.x / LPR;
   const int c = (threadIdx.x % LPR) * 4;
   if (i >= rows) return;
@@ -333,7 +597,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restric
     const int64_t at = static_cast<int64_t>(s) * rows + i;
     const float2 p = ml[at];
     if (p.y == 0.f) continue;
-    const float f = expf(p.x - m0);
+    const float f = LOG2 ? __builtin_amdgcn_exp2f(p.x - m0) : expf(p.x - m0);
     const float4 w = *reinterpret_cast<const float4*>(o + at * HD + c);
     L = fmaf(p.y, f, L);
     v[0] = fmaf(w.x, f, v[0]);
@@ -346,7 +610,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restric
   T* op = out + t * out_stride + h * HD + c;
 #pragma unroll
   for (int e = 0; e < 4; ++e) op[e] = from_f32<T>(v[e] * inv);
-  if (c == 0 && lse != nullptr) lse[static_cast<int64_t>(h) * Trows + t] = L == 0.f ? -INFINITY : M + logf(L);
+  if (c == 0 && lse != nullptr) lse[static_cast<int64_t>(h) * Trows + t] = L == 0.f ? -INFINITY : LOG2 ? (M + log2f(L)) * kLn2 : M + logf(L);
 }
 
 template <typename T>
@@ -355,10 +619,13 @@ hipError_t f32_dispatch(hipStream_t s, const PagedAttention& a, int64_t grid, in
   switch (a.hd) {
     case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16>, g, block, 0, s, a, tiles, splits);
     case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32>, g, block, 0, s, a, tiles, splits);
-    case 64: return launch(K_ATTENTION, paged_f32_kernel<T, 64>, g, block, 0, s, a, tiles, splits);
-    case 128: return launch(K_ATTENTION, paged_f32_kernel<T, 128>, g, block, 0, s, a, tiles, splits);
-    default: return hipErrorInvalidValue;
+    default: break;
   }
+  if constexpr (sizeof(T) == 4) {
+    if (a.hd == 64) return launch(K_ATTENTION, paged_f32_kernel<T, 64>, g, block, 0, s, a, tiles, splits);
+    if (a.hd == 128) return launch(K_ATTENTION, paged_f32_kernel<T, 128>, g, block, 0, s, a, tiles, splits);
+  }
+  return hipErrorInvalidValue;
 }
 
 template <typename T>
@@ -399,6 +666,11 @@ int paged_chunk(int max_len, int64_t workgroups, int* splits) {
 hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention& a, int max_rows, int splits) {
   const int tiles = (max_rows + 31) / 32;
   const int64_t grid = static_cast<int64_t>(splits) * tiles * (a.H / a.G) * a.B;
+  if (dtype == 1 && a.hd >= 64) {
+    const dim3 g(static_cast<uint32_t>(grid)), block(256);
+    if (a.hd == 64) return launch(K_ATTENTION, paged_few_kernel<64>, g, block, 0, s, a, tiles, splits);
+    return launch(K_ATTENTION, paged_few_kernel<128>, g, block, 0, s, a, tiles, splits);
+  }
   if (dtype == 1) return f32_dispatch<bf16_t>(s, a, grid, tiles, splits);
   return f32_dispatch<float>(s, a, grid, tiles, splits);
 }
