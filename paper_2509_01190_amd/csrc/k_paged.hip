@@ -18,6 +18,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "zsa_internal.h"
 
@@ -139,6 +140,15 @@ __device__ __forceinline__ Span span_of(const PagedAttention& a, int b) {
   return s;
 }
 
+// The parts of a row: (maximum, sum) in ml and the sums of values in o, one of
+// each split. A sum of kDone in the first says that the row is finished.
+constexpr float kDone = -1.0f;
+
+// the parts that another launch of the call has and this one has not
+__device__ __forceinline__ void empty_parts(const PagedAttention& a, int64_t at) {
+  for (int p = a.splits; p < a.parts; ++p) a.ml[at + static_cast<int64_t>(p) * a.T * a.H] = make_float2(-INFINITY, 0.f);
+}
+
 // the page ids and lengths, read as scalars: loads that would wait in line
 // with a wave's tile loads otherwise
 typedef const __attribute__((address_space(4))) int32_t* scalar_ids;
@@ -159,7 +169,7 @@ __device__ __forceinline__ scalar_ids scalar(const int32_t* p) {
 // as two bf16 numbers whose sum has 16 bits: the matrix cores have the time.
 template <int HD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2))) void paged_few_kernel(
-    PagedAttention a, int tiles, int splits) {
+    PagedAttention a, int tiles) {
   constexpr int NW = 4, KK = HD / 16, CT = HD / 32, CPR = HD / 8;
   constexpr int RB = HD * 2, HALF = 32 * RB;    // a tile of 32 rows of K, or V
   constexpr int RPL = 1024 / RB, NL = 16 / RPL;  // rows a load, loads per 16 rows
@@ -167,11 +177,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
   constexpr int SBYTES = NW * HD * HP * 4 > NW * 2 * HALF ? NW * HD * HP * 4 : NW * 2 * HALF;
   __shared__ __align__(1024) unsigned char smem[SBYTES];
   __shared__ float sm[NW][32], sl[NW][32];
-  const int split = blockIdx.x % splits, it0 = blockIdx.x / splits;
+  const int split = blockIdx.x % a.splits, it0 = blockIdx.x / a.splits;
   const int tile = it0 % tiles, gb = it0 / tiles, Hkv = a.H / a.G, g = gb % Hkv, b = gb / Hkv;
   const Span sp = span_of(a, b);
   const int i0 = tile * 32;
-  if (i0 >= sp.rows) return;
+  if (i0 >= sp.rows || sp.rows > a.few_rows) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int row = min(i0 + l32, sp.rows - 1);  // rows past the sequence are not stored
@@ -383,17 +393,451 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
       for (int e = 0; e < 4; ++e) v[e] = fmaf(f, so[(w * HD + c0 + e) * HP + q], v[e]);
     }
     const int t = sp.lo + i / a.G, h = g * a.G + i % a.G;
-    if (a.ml == nullptr) {
+    const int64_t row0 = static_cast<int64_t>(t) * a.H + h;
+    if (a.direct) {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
       *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + t * a.out_stride + h * HD + c0) =
           make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
       if (c0 == 0 && a.lse != nullptr)
         a.lse[static_cast<int64_t>(h) * a.T + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      if (c0 == 0 && a.ml != nullptr) a.ml[row0] = make_float2(0.f, kDone);
     } else {
-      const int64_t at = (static_cast<int64_t>(split) * a.T + t) * a.H + h;
-      if (c0 == 0) a.ml[at] = make_float2(m, l);
+      const int64_t at = static_cast<int64_t>(split) * a.T * a.H + row0;
+      if (c0 == 0) {
+        a.ml[at] = make_float2(m, l);
+        if (split == 0) empty_parts(a, at);
+      }
       if (l != 0.f) *reinterpret_cast<float4*>(a.o + at * HD + c0) = make_float4(v[0], v[1], v[2], v[3]);
     }
+  }
+}
+
+// bf16, heads of 64 and 128, many packed rows: bound by the products. A
+// workgroup takes 32 QB NW packed rows of one (sequence, key/value head) and a
+// split of its keys; all waves share the K and V tiles of 64 keys, three of
+// them in LDS, loaded two ahead straight from the pages. A wave owns 32 QB rows
+// and issues the products S(u + 1) = K Q^T and O += V P(u - 1) one at a time
+// between the exponentials of step u, relative to a reference maximum that
+// moves only when it must: the order of the work, the tile layout and the
+// reasons are those of attn_wide_kernel (k_attn.hip). What differs is where a
+// tile's rows come from and which keys a row sees.
+//  * A load instruction covers rows of one page (4 of 128, 8 of 64 columns);
+//    its page id is in a register of all lanes that holds the next 64 ids of
+//    the table, read 64 at a time: a scalar load would make every wait for LDS
+//    a wait for all of it, a vector load one for the tiles under way.
+//  * The resource ends with the sequence, so rows behind it read as zeros.
+//  * The packed rows put the G query heads that share a key/value head into
+//    one workgroup: its tiles are read once for all of them.
+template <int HD, int QB, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_many_kernel(
+    PagedAttention a, int tiles, int pairs) {
+  constexpr int WQ = 32 * QB, BQ = WQ * NW, BK = 64;
+  constexpr int KK = HD / 16, CT = HD / 32, CPR = HD / 8;
+  constexpr int RB = HD * 2, HALF = BK * RB, BUF = 2 * HALF, NB = 3, OLD = HD + 8;
+  constexpr int SBYTES = NB * BUF > NW * WQ * OLD * 2 ? NB * BUF : NW * WQ * OLD * 2;
+  constexpr int RPL = 1024 / RB, LPW = HALF / 1024 / NW;  // rows per load, loads per wave and operand
+  static_assert(LPW * NW * 1024 == HALF && NW * RPL % 16 == 0, "tile split");
+  __shared__ __align__(1024) unsigned char smem[SBYTES];
+
+  // the row blocks of a pair (split of the keys, key/value head, sequence) run
+  // on one XCD one after another, the last ones, which see most keys, first
+  const int pair = static_cast<int>(blockIdx.x >> 3) / tiles * 8 + (blockIdx.x & 7);
+  if (pair >= pairs) return;
+  const int tile = tiles - 1 - static_cast<int>(blockIdx.x >> 3) % tiles;
+  const int Hkv = a.H / a.G, split = pair / Hkv % a.splits, g = pair % Hkv, b = pair / Hkv / a.splits;
+  const Span sp = span_of(a, b);
+  const int i0 = tile * BQ;
+  if (i0 >= sp.rows || sp.rows <= a.few_rows) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, l32 = lane & 31;
+  const int wq0 = i0 + wave * WQ;  // the wave's first packed row
+  const float scale_log2 = a.scale * kLog2e;
+  // keys that packed row i sees
+  auto seen = [&](int i) { return a.causal ? min(sp.first + min(i, sp.rows - 1) / a.G, sp.len) : sp.len; };
+  const int k0 = split * a.chunk;
+  const int kend = min(seen(i0 + BQ - 1), k0 + a.chunk);
+  const int nt = max((kend - k0 + BK - 1) / BK, 0);
+  // the wave's own tiles: none past its last row's last key
+  const int wlast = min(seen(wq0 + WQ - 1), kend), wlim0 = seen(wq0);
+  const int ntw = min(nt, (wlast - k0 + BK - 1) / BK);
+
+  const uint32_t rowb = static_cast<uint32_t>(a.at.kvd) * 4u;
+  auto ksw = [](int r) { return HD == 64 ? (r >> 1) & 7 : r & 15; };
+  auto vsw = [](int r) { return HD == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; };
+  const int lrow = wave * RPL + lane / CPR;  // tile row of the wave's first load; the later ones are 16 n rows on
+  const uint32_t koff = (lane / CPR) * rowb + (((lane % CPR) ^ ksw(lrow)) << 4);
+  const uint32_t voff = (lane / CPR) * rowb + (((lane % CPR) ^ vsw(lrow)) << 4);
+  const uint32_t lds0 = lds_address(smem) + wave * 1024;
+  const char* pool = static_cast<const char*>(a.at.pool);
+  // ids of the 64 pages from `idp` on, one a lane, and of the 64 after them
+  const int most = sp.len > 0 ? (sp.len - 1) >> a.at.shift : 0;
+  int idp = k0 >> a.at.shift;
+  auto read_ids = [&](int from) { return sp.len > 0 ? sp.table[min(from + lane, most)] : -1; };
+  int ids = nt > 0 ? read_ids(idp) : -1, idn = nt > 0 ? read_ids(idp + 64) : -1;
+  auto load_rows = [&](int j, uint32_t lds) {  // K and V of RPL rows from row j on
+    const int p = j >> a.at.shift;
+    if (p >= idp + 64) {
+      asm volatile("" : "+v"(idn));  // waited for here
+      ids = idn;
+      idp += 64;
+      idn = read_ids(idp + 64);
+    }
+    const int page = __builtin_amdgcn_readlane(ids, p - idp);
+    const bool there = j < sp.len && page >= 0 && page < a.at.n_pages;
+    const uint32_t bytes = there ? static_cast<uint32_t>(min(sp.len - j, RPL)) * rowb - g * RB : 0u;
+    const char* at = pool + (there ? page : 0) * (a.at.page_stride * 2) +
+                     static_cast<uint32_t>(j & ((1 << a.at.shift) - 1)) * rowb + g * RB;
+    u32x4 kres = buffer_resource(at, bytes), vres = buffer_resource(at + rowb / 2, there ? bytes - rowb / 2 : 0u);
+    // a load in asm may follow a vector instruction's write of its scalar operands by five states at least
+    asm volatile("s_nop 4" : "+s"(kres), "+s"(vres));
+    lds_load16(lds, koff, kres);
+    lds_load16(lds + HALF, voff, vres);
+  };
+  auto load_tile = [&](int t, int buf) {
+#pragma unroll
+    for (int i = 0; i < LPW; ++i)
+      load_rows(k0 + t * BK + i * (NW * RPL) + wave * RPL, lds0 + buf * BUF + i * (NW * 1024));
+  };
+
+  float mu[QB], l_run[QB];  // reference max (scaled, exp2 units); sum over this lane's keys
+  f32x16_t o[QB][CT], sa[QB], sb[QB];
+  bf16x8_t pf[QB][2];  // P of the last step: [row block][16 keys]
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    l_run[qb] = 0.f;
+    mu[qb] = -1e30f;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[qb][ct][r] = 0.f;
+  }
+  int lim[QB];
+  const bf16_t* qrow[QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    // rows past the sequence are clamped, not zeroed: their outputs are not stored
+    const int i = min(wq0 + 32 * qb + l32, sp.rows - 1);
+    lim[qb] = seen(i);
+    qrow[qb] = static_cast<const bf16_t*>(a.q) + static_cast<int64_t>(sp.lo + i / a.G) * a.q_stride +
+               (g * a.G + i % a.G) * HD + half * 8;
+  }
+  bf16x8_t qf[QB][KK];
+  const f32x16_t zero = {};
+
+  if (nt > 0) {
+    load_tile(0, 0);
+    if (nt > 1) load_tile(1, 1);
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+        qf[qb][kk] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(qrow[qb] + kk * 16));
+
+    // fragment addresses within a tile: K rows l32 (+ 32), chunk 2 kk + half;
+    // V key rows 4 half + r (+ 8, 16 ..), the channel runs of a transposing read
+    const uint32_t kf0 = l32 * RB, vrow = 4 * half + ((lane & 15) >> 2);
+    const int ks0 = ksw(l32), vs0 = vsw(vrow);
+    const uint32_t vf0 = HALF + vrow * RB + (lane & 1) * 8;
+    const int vch = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+    uint32_t kaddr[KK], vaddr[CT];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) kaddr[kk] = kf0 + (((2 * kk + half) ^ ks0) << 4);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) vaddr[ct] = vf0 + (((4 * ct + vch) ^ vs0) << 4);
+    auto read_k = [&](const unsigned char* base, int kk) {
+      return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(base + kaddr[kk]));
+    };
+    auto read_v = [&](const unsigned char* base, int k, int ct) {
+      const unsigned char* vr = base + vaddr[ct] + k * (16 * RB);
+      return __builtin_bit_cast(bf16x8_t, lds_read_columns(vr, vr + 8 * RB));
+    };
+    auto row_max = [&](const f32x16_t& s) {
+      float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
+#pragma unroll
+      for (int r = 3; r < 15; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
+      return half_swap_max(fmaxf(mx, s[15]));
+    };
+    auto mask = [&](int u, f32x16_t (&s)[QB]) {
+      const int j0 = k0 + 32 * u;
+      if (j0 + 32 <= wlim0) return;
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        int left = lim[qb] - j0 - 4 * half;  // keys from this lane's limit on are masked
+        asm("" : "+v"(left));  // the comparisons stay here (hoisted, their masks fill the scalar registers)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (8 * (r >> 2) + (r & 3) >= left) s[qb][r] = -INFINITY;
+      }
+    };
+    // one step: the exponentials of step u (scores s) beside the products of
+    // O += V P(u - 1) and S(u + 1) = sn (the first step: alone)
+    auto step = [&](int u, int bufn, int ksn, int bufp, int ksp, f32x16_t (&s)[QB], f32x16_t (&sn)[QB], auto first_c) {
+      constexpr bool first = decltype(first_c)::value;
+      if (!first) mask(u, s);
+      constexpr int FA = 2;                                   // fragments in flight ahead of their use
+      constexpr int NF = KK + 2 * CT, NS = QB * NF;           // operand fragments, matrix instructions
+      constexpr int NU = 16 * QB;                             // pieces of vector work
+      const unsigned char* kp = smem + bufn * BUF + ksn * (32 * RB);
+      const unsigned char* vp = smem + bufp * BUF + ksp * (32 * RB);
+      bf16x8_t fr[FA + 1];
+      auto read = [&](int f) { fr[f % (FA + 1)] = f < KK ? read_k(kp, f) : read_v(vp, (f - KK) / CT, (f - KK) % CT); };
+      auto product = [&](int i) {
+        const int f = i / QB, qb = i % QB;
+        if (f < KK)
+          sn[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % (FA + 1)], qf[qb][f], f == 0 ? zero : sn[qb], 0, 0, 0);
+        else
+          o[qb][(f - KK) % CT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              fr[f % (FA + 1)], pf[qb][(f - KK) / CT], o[qb][(f - KK) % CT], 0, 0, 0);
+      };
+      float rsum[QB], a0 = 0.f, a1 = 0.f, p0 = 0.f, p1 = 0.f;
+      u32x4 pn[QB][2];
+      auto work = [&](int w) {
+        const int qb = w >> 4, r = w & 14;
+        if ((w & 1) == 0) {
+          p0 = __builtin_amdgcn_exp2f(fmaf(s[qb][r], scale_log2, -mu[qb]));
+          p1 = __builtin_amdgcn_exp2f(fmaf(s[qb][r + 1], scale_log2, -mu[qb]));
+          asm volatile("" : "+v"(p0), "+v"(p1));  // computed here, beside this step's products
+        } else {
+          uint32_t pw = pack_bf16x2(p0, p1);
+          a0 = r == 0 ? p0 : a0 + p0;
+          a1 = r == 0 ? p1 : a1 + p1;
+          asm volatile("" : "+v"(pw), "+v"(a0), "+v"(a1));
+          pn[qb][r >> 3][(r >> 1) & 3] = pw;
+          if (r == 14) rsum[qb] = a0 + a1;
+        }
+      };
+      if constexpr (first) {
+#pragma unroll
+        for (int k = 0; k < NU; ++k) work(k);
+      } else {
+#pragma unroll
+        for (int f = 0; f < FA; ++f) read(f);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          if (i % QB == 0 && i / QB + FA < NF) read(i / QB + FA);
+          product(i);
+#pragma unroll
+          for (int k = NU * i / NS; k < NU * (i + 1) / NS; ++k) work(k);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      bool high = false;
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) high |= !(rsum[qb] <= 4096.f);
+      if (!first && __builtin_amdgcn_ballot_w64(high) != 0) {
+        // a score far above the reference, or the first key that a row sees:
+        // move it, and redo this step's P
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const float m_new = fmaxf(mu[qb], row_max(s[qb]) * scale_log2);
+          const float alpha = __builtin_amdgcn_exp2f(mu[qb] - m_new);
+          mu[qb] = m_new;
+          l_run[qb] *= alpha;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[qb][ct][r] *= alpha;
+          rsum[qb] = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            const float e0 = __builtin_amdgcn_exp2f(fmaf(s[qb][r], scale_log2, -m_new));
+            const float e1 = __builtin_amdgcn_exp2f(fmaf(s[qb][r + 1], scale_log2, -m_new));
+            rsum[qb] += e0 + e1;
+            pn[qb][r >> 3][(r >> 1) & 3] = pack_bf16x2(e0, e1);
+          }
+        }
+      }
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        l_run[qb] += rsum[qb];
+        pf[qb][0] = __builtin_bit_cast(bf16x8_t, pn[qb][0]);
+        pf[qb][1] = __builtin_bit_cast(bf16x8_t, pn[qb][1]);
+      }
+    };
+
+    int bp = 2, bc = 0, bn = 1;  // buffers of tiles t - 1, t, t + 1
+    auto turn = [&]() {
+      const int f = bp;
+      bp = bc;
+      bc = bn;
+      bn = f;
+    };
+    turn_over();
+    // the first tile's scores, and the reference: the max over its 64 keys
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const bf16x8_t a0 = read_k(smem, kk), a1 = read_k(smem + 32 * RB, kk);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        sa[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, qf[qb][kk], kk == 0 ? zero : sa[qb], 0, 0, 0);
+        sb[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, qf[qb][kk], kk == 0 ? zero : sb[qb], 0, 0, 0);
+      }
+    }
+    mask(0, sa);
+    mask(1, sb);
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+      mu[qb] = fmaxf(fmaxf(row_max(sa[qb]), row_max(sb[qb])) * scale_log2, -1e30f);
+    step(0, bc, 1, bp, 1, sa, sb, std::true_type());
+    if (nt > 2) load_tile(2, bp);
+    step(1, bn, 0, bc, 0, sb, sa, std::false_type());
+    int t = 1;
+    for (; t < ntw; ++t) {
+      turn();
+      step(2 * t, bc, 1, bp, 1, sa, sb, std::false_type());
+      turn_over();
+      if (t + 2 < nt) load_tile(t + 2, bp);
+      step(2 * t + 1, bn, 0, bc, 0, sb, sa, std::false_type());
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const bf16x8_t v = read_v(smem + bc * BUF + 32 * RB, k, ct);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+          o[qb][ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[qb][k], o[qb][ct], 0, 0, 0);
+      }
+    for (; t < nt; ++t) {  // the tiles of the block's later rows
+      turn();
+      turn_over();
+      if (t + 2 < nt) load_tile(t + 2, bp);
+    }
+    turn_over();  // every wave is past the tiles before the output staging reuses them
+  }
+
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) l_run[qb] = half_swap_sum(l_run[qb]);
+  // A value that is not finite must not reach a row that does not see its key;
+  // through the product with its zero probability it has, and left a NaN.
+  // Where the wave's tiles hold hidden keys and its results a NaN, its rows are
+  // computed again, the second product on the vector ALU, key by key.
+  if (wlim0 < min(sp.len, k0 + max(ntw, 1) * BK)) {
+    bool odd = false;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) odd |= o[qb][ct][r] != o[qb][ct][r];
+    if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+      auto row_of = [&](int j) {  // row j's keys, or null
+        const int page = j < sp.len ? sp.table[j >> a.at.shift] : -1;
+        return page < 0 || page >= a.at.n_pages
+                   ? nullptr
+                   : pool + page * (a.at.page_stride * 2) + static_cast<uint32_t>(j & ((1 << a.at.shift) - 1)) * rowb + g * RB;
+      };
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        float m = -1e30f, l = 0.f;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[qb][ct][r] = 0.f;
+        for (int j0 = k0; j0 < wlast; j0 += 32) {
+          const char* kr = row_of(j0 + l32);
+          f32x16_t s = zero;
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk) {
+            u32x4 k = {0u, 0u, 0u, 0u};
+            if (kr != nullptr) k = *reinterpret_cast<const u32x4*>(kr + kk * 32 + half * 16);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), qf[qb][kk], s, 0, 0, 0);
+          }
+          float mx = m;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            if (j0 + 8 * (r >> 2) + 4 * half + (r & 3) >= lim[qb]) s[r] = -INFINITY;
+            mx = fmaxf(mx, s[r] * scale_log2);
+          }
+          mx = half_swap_max(mx);
+          const float alpha = __builtin_amdgcn_exp2f(m - mx);
+          m = mx;
+          l *= alpha;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[qb][ct][r] *= alpha;
+          float part = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale_log2, -m));
+            part += s[r];
+          }
+          l += half_swap_sum(part);
+#pragma unroll
+          for (int kk = 0; kk < 32; ++kk) {
+            // key j0 + kk: register (kk / 8) * 4 + kk % 4 of lane half (kk / 4) % 2
+            const float p = __shfl(s[(kk >> 3) * 4 + (kk & 3)], l32 + 32 * ((kk >> 2) & 1), 64);
+            const char* vr = j0 + kk < lim[qb] ? row_of(j0 + kk) : nullptr;
+            if (vr != nullptr) {
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                  const uint2 w = *reinterpret_cast<const uint2*>(vr + rowb / 2 + (ct * 32 + 2 * r + 4 * half) * 2);
+                  o[qb][ct][r] = fmaf(p, __uint_as_float(w.x << 16), o[qb][ct][r]);
+                  o[qb][ct][r + 1] = fmaf(p, __uint_as_float(w.x & 0xffff0000u), o[qb][ct][r + 1]);
+                  o[qb][ct][r + 2] = fmaf(p, __uint_as_float(w.y << 16), o[qb][ct][r + 2]);
+                  o[qb][ct][r + 3] = fmaf(p, __uint_as_float(w.y & 0xffff0000u), o[qb][ct][r + 3]);
+                }
+            }
+          }
+        }
+        mu[qb] = m;
+        l_run[qb] = l;
+      }
+    }
+  }
+
+  // o[qb][ct][r] = O^T[channel ct*32 + 8 (r/4) + 4 half + r%4][packed row wq0 + 32 qb + l32]
+  if (!a.direct) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int i = wq0 + 32 * qb + l32;
+      if (i >= sp.rows) continue;
+      const int64_t at = (static_cast<int64_t>(split) * a.T + sp.lo + i / a.G) * a.H + g * a.G + i % a.G;
+      if (half == 0) {
+        a.ml[at] = make_float2(l_run[qb] == 0.f ? -INFINITY : mu[qb], l_run[qb]);
+        if (split == 0) empty_parts(a, at);
+      }
+      if (l_run[qb] == 0.f) continue;
+      float* op = a.o + at * HD + 4 * half;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<float4*>(op + ct * 32 + 2 * r) =
+              make_float4(o[qb][ct][r], o[qb][ct][r + 1], o[qb][ct][r + 2], o[qb][ct][r + 3]);
+    }
+    return;
+  }
+  bf16_t* Os = reinterpret_cast<bf16_t*>(smem) + wave * WQ * OLD;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const float inv_l = l_run[qb] == 0.f ? 0.f : 1.0f / l_run[qb];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const uint2 w = {pack_bf16x2(o[qb][ct][r] * inv_l, o[qb][ct][r + 1] * inv_l),
+                         pack_bf16x2(o[qb][ct][r + 2] * inv_l, o[qb][ct][r + 3] * inv_l)};
+        *reinterpret_cast<uint2*>(Os + (32 * qb + l32) * OLD + ct * 32 + 2 * r + 4 * half) = w;
+      }
+    const int i = wq0 + 32 * qb + l32;
+    if (a.lse != nullptr && half == 0 && i < sp.rows)
+      a.lse[static_cast<int64_t>(g * a.G + i % a.G) * a.T + sp.lo + i / a.G] =
+          l_run[qb] == 0.f ? -INFINITY : (mu[qb] + log2f(l_run[qb])) * kLn2;
+    if (a.ml != nullptr && half == 0 && i < sp.rows)
+      a.ml[static_cast<int64_t>(sp.lo + i / a.G) * a.H + g * a.G + i % a.G] = make_float2(0.f, kDone);
+  }
+  // each wave stores its own rows: its LDS writes are in order before its reads
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  for (int c = lane; c < WQ * CPR; c += 64) {
+    const int r = c / CPR, ch = (c % CPR) * 8, i = wq0 + r;
+    if (i < sp.rows)
+      *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.out) + static_cast<int64_t>(sp.lo + i / a.G) * a.out_stride +
+                                (g * a.G + i % a.G) * HD + ch) = *reinterpret_cast<const u32x4*>(Os + r * OLD + ch);
   }
 }
 
@@ -404,13 +848,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
 // take the split's 32-key tiles in turn and their (max, sum, O) are merged
 // through LDS in wave order.
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void paged_f32_kernel(PagedAttention a, int tiles, int splits) {
+__global__ __launch_bounds__(256) void paged_f32_kernel(PagedAttention a, int tiles) {
   constexpr int NW = 4, KK = HD / 8;
   constexpr int CT = HD < 32 ? 1 : HD / 32;  // 32-channel blocks of O (half empty at HD 16)
   constexpr int HP = 33;                     // merge row stride: [channel][query]
   __shared__ float so[NW][HD * HP];
   __shared__ float sm[NW][32], sl[NW][32];
-  const int split = blockIdx.x % splits, it0 = blockIdx.x / splits;
+  const int split = blockIdx.x % a.splits, it0 = blockIdx.x / a.splits;
   const int tile = it0 % tiles, gb = it0 / tiles, g = gb % (a.H / a.G), b = gb / (a.H / a.G);
   const Span sp = span_of(a, b);
   const int i0 = tile * 32;
@@ -561,15 +1005,19 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedAttention a, int ti
       for (int e = 0; e < 4; ++e) v[e] = fmaf(f, so[w][(c0 + e) * HP + q], v[e]);
     }
     const int t = sp.lo + i / a.G, h = g * a.G + i % a.G;
-    if (a.ml == nullptr) {
+    const int64_t row0 = static_cast<int64_t>(t) * a.H + h;
+    if (a.direct) {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
       T* op = static_cast<T*>(a.out) + t * a.out_stride + h * HD + c0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) op[e] = from_f32<T>(v[e] * inv);
       if (c0 == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(h) * a.T + t] = l == 0.f ? -INFINITY : m + logf(l);
     } else {
-      const int64_t at = (static_cast<int64_t>(split) * a.T + t) * a.H + h;
-      if (c0 == 0) a.ml[at] = make_float2(m, l);
+      const int64_t at = static_cast<int64_t>(split) * a.T * a.H + row0;
+      if (c0 == 0) {
+        a.ml[at] = make_float2(m, l);
+        if (split == 0) empty_parts(a, at);
+      }
       if (l != 0.f) *reinterpret_cast<float4*>(a.o + at * HD + c0) = make_float4(v[0], v[1], v[2], v[3]);
     }
   }
@@ -589,6 +1037,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restric
   const int64_t i = static_cast<int64_t>(blockIdx.x) * (256 / LPR) + threadIdx.x / LPR;
   const int c = (threadIdx.x % LPR) * 4;
   if (i >= rows) return;
+  if (ml[i].y == kDone) return;
   float M = -INFINITY;
   for (int s = 0; s < parts; ++s) M = fmaxf(M, ml[static_cast<int64_t>(s) * rows + i].x);
   const float m0 = M == -INFINITY ? 0.f : M;
@@ -614,16 +1063,16 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restric
 }
 
 template <typename T>
-hipError_t f32_dispatch(hipStream_t s, const PagedAttention& a, int64_t grid, int tiles, int splits) {
-  const dim3 g(static_cast<uint32_t>(grid)), block(256);
+hipError_t f32_dispatch(hipStream_t s, const PagedAttention& a, dim3 g, int tiles) {
+  const dim3 block(256);
   switch (a.hd) {
-    case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16>, g, block, 0, s, a, tiles, splits);
-    case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32>, g, block, 0, s, a, tiles, splits);
+    case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16>, g, block, 0, s, a, tiles);
+    case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32>, g, block, 0, s, a, tiles);
     default: break;
   }
   if constexpr (sizeof(T) == 4) {
-    if (a.hd == 64) return launch(K_ATTENTION, paged_f32_kernel<T, 64>, g, block, 0, s, a, tiles, splits);
-    if (a.hd == 128) return launch(K_ATTENTION, paged_f32_kernel<T, 128>, g, block, 0, s, a, tiles, splits);
+    if (a.hd == 64) return launch(K_ATTENTION, paged_f32_kernel<T, 64>, g, block, 0, s, a, tiles);
+    if (a.hd == 128) return launch(K_ATTENTION, paged_f32_kernel<T, 128>, g, block, 0, s, a, tiles);
   }
   return hipErrorInvalidValue;
 }
@@ -654,25 +1103,36 @@ hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a) {
   return launch(K_MISC, paged_append_kernel<float>, grid, block, 0, s, a, rows);
 }
 
-// Splits of the keys: enough workgroups for four a CU, none of fewer than 128 keys.
-int paged_chunk(int max_len, int64_t workgroups, int* splits) {
-  const int blocks = std::max(1, (max_len + 127) / 128);
-  const int64_t want = std::max<int64_t>(1, 4 * static_cast<int64_t>(device_cu_count()) / std::max<int64_t>(workgroups, 1));
-  const int per = static_cast<int>((blocks + std::min<int64_t>(want, blocks) - 1) / std::min<int64_t>(want, blocks));
-  *splits = (blocks + per - 1) / per;
-  return per * 128;
+bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 64; }
+
+// Splits of the keys. The few-row kernels: enough workgroups for four a CU, of
+// 128 keys at least. The many-row kernel: two a CU, of 512 keys at least (a
+// split's part is as many bytes as 256 of its keys).
+int paged_chunk(bool many, int max_len, int64_t workgroups, int* splits) {
+  const int least = many ? 512 : 128;
+  const int64_t blocks = std::max(1, (max_len + least - 1) / least), wgs = std::max<int64_t>(workgroups, 1);
+  const int64_t want = std::min(blocks, std::max<int64_t>(1, ((many ? 2 : 4) * static_cast<int64_t>(device_cu_count()) + wgs - 1) / wgs));
+  const int per = static_cast<int>((blocks + want - 1) / want);
+  *splits = static_cast<int>((blocks + per - 1) / per);
+  return per * least;
 }
 
-hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention& a, int max_rows, int splits) {
-  const int tiles = (max_rows + 31) / 32;
-  const int64_t grid = static_cast<int64_t>(splits) * tiles * (a.H / a.G) * a.B;
-  if (dtype == 1 && a.hd >= 64) {
-    const dim3 g(static_cast<uint32_t>(grid)), block(256);
-    if (a.hd == 64) return launch(K_ATTENTION, paged_few_kernel<64>, g, block, 0, s, a, tiles, splits);
-    return launch(K_ATTENTION, paged_few_kernel<128>, g, block, 0, s, a, tiles, splits);
+hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention& a, bool many, int max_rows) {
+  const int64_t pairs = static_cast<int64_t>(a.splits) * (a.H / a.G) * a.B;
+  if (many) {
+    const int tiles = (max_rows + kPagedManyRows - 1) / kPagedManyRows;
+    const dim3 g(static_cast<uint32_t>((pairs + 7) / 8 * 8 * tiles));
+    if (a.hd == 64) return launch(K_ATTENTION, paged_many_kernel<64, 2, 4>, g, dim3(256), 0, s, a, tiles, static_cast<int>(pairs));
+    return launch(K_ATTENTION, paged_many_kernel<128, 1, 8>, g, dim3(512), 0, s, a, tiles, static_cast<int>(pairs));
   }
-  if (dtype == 1) return f32_dispatch<bf16_t>(s, a, grid, tiles, splits);
-  return f32_dispatch<float>(s, a, grid, tiles, splits);
+  const int tiles = (max_rows + 31) / 32;
+  const dim3 g(static_cast<uint32_t>(pairs * tiles));
+  if (paged_matrix(dtype, a.hd)) {
+    if (a.hd == 64) return launch(K_ATTENTION, paged_few_kernel<64>, g, dim3(256), 0, s, a, tiles);
+    return launch(K_ATTENTION, paged_few_kernel<128>, g, dim3(256), 0, s, a, tiles);
+  }
+  if (dtype == 1) return f32_dispatch<bf16_t>(s, a, g, tiles);
+  return f32_dispatch<float>(s, a, g, tiles);
 }
 
 hipError_t launch_paged_join(hipStream_t s, int dtype, const float2* ml, const float* o, int parts, int T, int H,

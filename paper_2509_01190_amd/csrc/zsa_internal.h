@@ -460,17 +460,22 @@ struct PagedAttention {
   int T, B, H, G, hd;
   int causal;
   float scale;
-  int chunk;                  // keys a split takes, a multiple of 128
-  void* out;                  // finished rows, when one split covers everything (ml null)
+  int few_rows;               // a few-row launch takes the sequences of up to so many packed rows, a many-row one the others
+  int chunk, splits;          // keys a split takes, a multiple of 128; splits
+  int parts;                  // the call's parts from this launch's first on
+  int direct;                 // one split, and no other part: rows are finished here
+  void* out;
   int64_t out_stride;
   float* lse;                 // [H][T] or null
-  float2* ml;                 // [split][T * H] maximum and sum of the scores, else
-  float* o;                   // [split][T * H][hd] sums of values
+  float2* ml;                 // [part][T * H] maximum and sum of the scores, or null: no row has parts
+  float* o;                   // [part][T * H][hd] sums of values
 };
+constexpr int kPagedManyRows = 256;  // packed rows of the many-row kernel's workgroup
+bool paged_matrix(int dtype, int hd);  // the bf16 matrix kernels take these heads: one for few rows, one for many
 // keys a split of up to max_len rows takes, and how many splits that makes
-int paged_chunk(int max_len, int64_t workgroups, int* splits);
-// max_rows: packed rows of the longest sequence
-hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention& a, int max_rows, int splits);
+int paged_chunk(bool many, int max_len, int64_t workgroups, int* splits);
+// max_rows: packed rows of the longest sequence of the launch
+hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention& a, bool many, int max_rows);
 hipError_t launch_paged_join(hipStream_t s, int dtype, const float2* ml, const float* o, int parts, int T, int H,
                              int hd, void* out, int64_t out_stride, float* lse);
 

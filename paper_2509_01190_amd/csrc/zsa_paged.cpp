@@ -81,21 +81,54 @@ size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
   return round256(parts * rows * sizeof(float2)) + round256(parts * rows * hd * sizeof(float));
 }
 
-// The splits of a call's own rows and of the common prefix (0: none).
-struct Plan {
-  int chunk, splits;    // of the sequences' own rows
-  int pchunk, psplits;  // of the prefix
-  int parts() const { return psplits + splits; }
-  bool direct() const { return parts() == 1; }
+// Packed rows (new rows times query heads per key/value head) up to which a
+// sequence goes to the few-row kernel.
+constexpr int kFewRows = 64;
+
+struct Launch {
+  bool many;
+  int max_rows;       // packed rows of its longest sequence; 0: nothing to launch
+  int chunk, splits;
 };
 
-Plan plan_of(int dtype, int hd, int H, int Hkv, int batch, int max_new, int T, int max_len, int prefix) {
+// What a call launches: over the common prefix, over the own rows of the
+// sequences of few packed rows, and of those of many. The parts of the prefix
+// come first, the others' after them, in the same places.
+struct Plan {
+  Launch prefix, few, many;
+  int own() const { return std::max(few.splits, many.splits); }
+  int parts() const { return prefix.splits + own(); }
+  // a launch finishes its rows itself where they have no other part
+  bool direct(const Launch& l) const { return prefix.splits == 0 && l.splits == 1; }
+  bool join() const { return parts() > 1; }
+};
+
+Launch launch_of(bool many, int64_t max_rows, int64_t tiles, int max_len) {
+  Launch l{};
+  l.many = many;
+  l.max_rows = static_cast<int>(max_rows);
+  l.chunk = zsa::paged_chunk(many, max_len, tiles, &l.splits);
+  return l;
+}
+
+Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int max_len, int prefix) {
   Plan p{};
-  const int G = H / Hkv;
-  const int64_t rows = std::min<int64_t>(static_cast<int64_t>(max_new) * G, 1 << 30);
-  p.chunk = zsa::paged_chunk(max_len, (rows + 31) / 32 * Hkv * batch, &p.splits);
-  if (prefix > 0)
-    p.pchunk = zsa::paged_chunk(prefix, (static_cast<int64_t>(T) * G + 31) / 32 * Hkv, &p.psplits);
+  const int64_t G = H / kv.n_kv_heads, T = cu[batch];
+  const bool matrix = zsa::paged_matrix(kv.dtype, kv.head_dim);
+  int64_t most[2] = {0, 0}, tiles[2] = {0, 0};
+  for (int b = 0; b < batch; ++b) {
+    const int64_t rows = (cu[b + 1] - cu[b]) * G;
+    const int many = matrix && rows > kFewRows, tile = many ? zsa::kPagedManyRows : 32;
+    most[many] = std::max(most[many], rows);
+    tiles[many] += (rows + tile - 1) / tile;
+  }
+  if (most[0] > 0) p.few = launch_of(false, most[0], tiles[0] * kv.n_kv_heads, max_len);
+  if (most[1] > 0) p.many = launch_of(true, most[1], tiles[1] * kv.n_kv_heads, max_len);
+  if (prefix > 0) {
+    const bool many = matrix && T * G > kFewRows;
+    const int tile = many ? zsa::kPagedManyRows : 32;
+    p.prefix = launch_of(many, T * G, (T * G + tile - 1) / tile * kv.n_kv_heads, prefix);
+  }
   return p;
 }
 
@@ -130,12 +163,15 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
     if (ws_bytes < need) return set_error(ZSA_EWORKSPACE, "workspace %zu bytes < %zu", ws_bytes, need);
   }
   if (T == 0) return ZSA_OK;
-  const Plan p = plan_of(kv->dtype, kv->head_dim, n_heads, kv->n_kv_heads, batch, max_new, T, max_kv_len, prefix_len);
+  const Plan p = plan_of(*kv, n_heads, batch, cu_host, max_kv_len, prefix_len);
+  for (const Launch* l : {&p.prefix, &p.few, &p.many})
+    if (static_cast<int64_t>(l->splits) * ((l->max_rows + 31) / 32) * kv->n_kv_heads * (l == &p.prefix ? 1 : batch) > (1 << 23))
+      return set_error(ZSA_EUNSUPPORTED, "%d sequences of up to %d rows of %d heads: more workgroups than a grid holds",
+                       batch, max_new, n_heads);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int64_t rows = static_cast<int64_t>(T) * n_heads;
-  float2* ml = p.direct() ? nullptr : static_cast<float2*>(ws);
-  float* o = p.direct() ? nullptr
-                        : reinterpret_cast<float*>(static_cast<char*>(ws) + round256(p.parts() * rows * sizeof(float2)));
+  float2* ml = p.join() ? static_cast<float2*>(ws) : nullptr;
+  float* o = p.join() ? reinterpret_cast<float*>(static_cast<char*>(ws) + round256(p.parts() * rows * sizeof(float2))) : nullptr;
   zsa::PagedAttention a{};
   a.at = rows_of(*kv);
   a.q = q;
@@ -150,13 +186,22 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
   a.hd = kv->head_dim;
   a.causal = causal != 0;
   a.scale = scale;
-  a.chunk = p.chunk;
   a.out = out;
   a.out_stride = out_stride;
   a.lse = lse;
-  a.ml = ml;
-  a.o = o;
-  if (p.psplits > 0) {
+  auto go = [&](zsa::PagedAttention x, const Launch& l, int part, bool direct) {
+    x.few_rows = l.many ? (x.cu != nullptr ? kFewRows : 0) : (p.many.splits > 0 && x.cu != nullptr ? kFewRows : INT32_MAX);
+    x.chunk = l.chunk;
+    x.splits = l.splits;
+    x.parts = part == 0 && x.cu == nullptr ? l.splits : p.own();
+    x.direct = direct;
+    if (ml != nullptr) {
+      x.ml = ml + part * rows;
+      x.o = o + part * rows * kv->head_dim;
+    }
+    return zsa::launch_paged_attention(s, kv->dtype, x, l.many, l.max_rows);
+  };
+  if (p.prefix.splits > 0) {
     zsa::PagedAttention f = a;
     f.at.table = prefix_pages;
     f.at.max_pages = static_cast<int>((static_cast<int64_t>(prefix_len) + kv->page_size - 1) / kv->page_size);
@@ -165,13 +210,11 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
     f.max_len = prefix_len;
     f.B = 1;
     f.causal = 0;
-    f.chunk = p.pchunk;
-    HIP_TRY(zsa::launch_paged_attention(s, kv->dtype, f, T * G, p.psplits), "prefix attention");
-    a.ml = ml + p.psplits * rows;
-    a.o = o + p.psplits * rows * kv->head_dim;
+    HIP_TRY(go(f, p.prefix, 0, false), "prefix attention");
   }
-  HIP_TRY(zsa::launch_paged_attention(s, kv->dtype, a, max_new * G, p.splits), "paged attention");
-  if (ml != nullptr)
+  if (p.many.splits > 0) HIP_TRY(go(a, p.many, p.prefix.splits, p.direct(p.many)), "paged attention");
+  if (p.few.splits > 0) HIP_TRY(go(a, p.few, p.prefix.splits, p.direct(p.few)), "paged attention");
+  if (p.join())
     HIP_TRY(zsa::launch_paged_join(s, kv->dtype, ml, o, p.parts(), T, n_heads, kv->head_dim, out, out_stride, lse),
             "paged attention's parts");
   return ZSA_OK;
@@ -237,12 +280,10 @@ size_t zsa_paged_attention_workspace_size(const zsa_paged_kv* kv, int32_t n_head
   if (kv == nullptr || cu_host == nullptr || batch <= 0 || n_heads <= 0 || kv->n_kv_heads <= 0 ||
       n_heads % kv->n_kv_heads != 0 || max_kv_len < 0 || prefix_len < 0)
     return 0;
-  int max_new = 0;
-  for (int b = 0; b < batch; ++b) max_new = std::max(max_new, cu_host[b + 1] - cu_host[b]);
   const int T = cu_host[batch];
   if (T <= 0) return 0;
-  const Plan p = plan_of(kv->dtype, kv->head_dim, n_heads, kv->n_kv_heads, batch, max_new, T, max_kv_len, prefix_len);
-  return p.direct() ? 0 : parts_bytes(p.parts(), static_cast<int64_t>(T) * n_heads, kv->head_dim);
+  const Plan p = plan_of(*kv, n_heads, batch, cu_host, max_kv_len, prefix_len);
+  return !p.join() ? 0 : parts_bytes(p.parts(), static_cast<int64_t>(T) * n_heads, kv->head_dim);
 }
 
 int zsa_paged_attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_heads,
