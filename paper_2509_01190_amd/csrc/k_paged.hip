@@ -140,6 +140,13 @@ __device__ __forceinline__ Span span_of(const PagedAttention& a, int b) {
   return s;
 }
 
+// A launch's work: the common prefix's and the sequences' own, if both are of
+// one kind. The prefix's workgroups, which have more to do, come first.
+struct PagedJobs {
+  PagedAttention job[2];
+  uint32_t first;  // workgroups of the first
+};
+
 // The parts of a row: (maximum, sum) in ml and the sums of values in o, one of
 // each split. A sum of kDone in the first says that the row is finished.
 constexpr float kDone = -1.0f;
@@ -169,7 +176,7 @@ __device__ __forceinline__ scalar_ids scalar(const int32_t* p) {
 // as two bf16 numbers whose sum has 16 bits: the matrix cores have the time.
 template <int HD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2))) void paged_few_kernel(
-    PagedAttention a, int tiles) {
+    PagedJobs jobs) {
   constexpr int NW = 4, KK = HD / 16, CT = HD / 32, CPR = HD / 8;
   constexpr int RB = HD * 2, HALF = 32 * RB;    // a tile of 32 rows of K, or V
   constexpr int RPL = 1024 / RB, NL = 16 / RPL;  // rows a load, loads per 16 rows
@@ -177,8 +184,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
   constexpr int SBYTES = NW * HD * HP * 4 > NW * 2 * HALF ? NW * HD * HP * 4 : NW * 2 * HALF;
   __shared__ __align__(1024) unsigned char smem[SBYTES];
   __shared__ float sm[NW][32], sl[NW][32];
-  const int split = blockIdx.x % a.splits, it0 = blockIdx.x / a.splits;
-  const int tile = it0 % tiles, gb = it0 / tiles, Hkv = a.H / a.G, g = gb % Hkv, b = gb / Hkv;
+  const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
+  const PagedAttention& a = jobs.job[which];
+  const int split = block % a.splits, it0 = block / a.splits;
+  const int tile = it0 % a.tiles, gb = it0 / a.tiles, Hkv = a.H / a.G, g = gb % Hkv, b = gb / Hkv;
   const Span sp = span_of(a, b);
   const int i0 = tile * 32;
   if (i0 >= sp.rows || sp.rows > a.few_rows) return;
@@ -430,7 +439,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
 //    one workgroup: its tiles are read once for all of them.
 template <int HD, int QB, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_many_kernel(
-    PagedAttention a, int tiles, int pairs) {
+    PagedJobs jobs) {
   constexpr int WQ = 32 * QB, BQ = WQ * NW, BK = 64;
   constexpr int KK = HD / 16, CT = HD / 32, CPR = HD / 8;
   constexpr int RB = HD * 2, HALF = BK * RB, BUF = 2 * HALF, NB = 3, OLD = HD + 8;
@@ -441,10 +450,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
   // the row blocks of a pair (split of the keys, key/value head, sequence) run
   // on one XCD one after another, the last ones, which see most keys, first
-  const int pair = static_cast<int>(blockIdx.x >> 3) / tiles * 8 + (blockIdx.x & 7);
-  if (pair >= pairs) return;
-  const int tile = tiles - 1 - static_cast<int>(blockIdx.x >> 3) % tiles;
-  const int Hkv = a.H / a.G, split = pair / Hkv % a.splits, g = pair % Hkv, b = pair / Hkv / a.splits;
+  const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
+  const PagedAttention& a = jobs.job[which];
+  const int Hkv = a.H / a.G, pair = (block >> 3) / a.tiles * 8 + (block & 7);
+  if (pair >= a.splits * Hkv * a.B) return;
+  const int tile = a.tiles - 1 - (block >> 3) % a.tiles;
+  const int split = pair / Hkv % a.splits, g = pair % Hkv, b = pair / Hkv / a.splits;
   const Span sp = span_of(a, b);
   const int i0 = tile * BQ;
   if (i0 >= sp.rows || sp.rows <= a.few_rows) return;
@@ -848,14 +859,16 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // take the split's 32-key tiles in turn and their (max, sum, O) are merged
 // through LDS in wave order.
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void paged_f32_kernel(PagedAttention a, int tiles) {
+__global__ __launch_bounds__(256) void paged_f32_kernel(PagedJobs jobs) {
   constexpr int NW = 4, KK = HD / 8;
   constexpr int CT = HD < 32 ? 1 : HD / 32;  // 32-channel blocks of O (half empty at HD 16)
   constexpr int HP = 33;                     // merge row stride: [channel][query]
   __shared__ float so[NW][HD * HP];
   __shared__ float sm[NW][32], sl[NW][32];
-  const int split = blockIdx.x % a.splits, it0 = blockIdx.x / a.splits;
-  const int tile = it0 % tiles, gb = it0 / tiles, g = gb % (a.H / a.G), b = gb / (a.H / a.G);
+  const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
+  const PagedAttention& a = jobs.job[which];
+  const int split = block % a.splits, it0 = block / a.splits;
+  const int tile = it0 % a.tiles, gb = it0 / a.tiles, g = gb % (a.H / a.G), b = gb / (a.H / a.G);
   const Span sp = span_of(a, b);
   const int i0 = tile * 32;
   if (i0 >= sp.rows) return;
@@ -1024,55 +1037,91 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedAttention a, int ti
 }
 
 // The parts of every row, joined: M = max m, L = sum l exp(m - M), out = sum o
-// exp(m - M) / L, in the splits' order. A part without keys has l = 0 and no o.
-// A thread takes four channels. (The bf16 matrix kernels' maxima are in units
-// of log 2, as they used them.)
+// exp(m - M) / L. A part without keys has l = 0 and no o. (The bf16 matrix
+// kernels' maxima are in units of log 2, as they used them.) HD / 4 threads
+// take four channels each of a row's parts sub, sub + per, ...; `per` such
+// groups a row, whose sums are added in their order. Few rows of many parts
+// need them: 128 rows of 62 parts with one group 39.7 us.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restrict__ ml,
                                                          const float* __restrict__ o, int parts, int rows,
                                                          int H, int Trows, T* __restrict__ out,
-                                                         int64_t out_stride, float* __restrict__ lse) {
-  constexpr int LPR = HD / 4;  // threads a row
+                                                         int64_t out_stride, float* __restrict__ lse, int per) {
+  constexpr int LPR = HD / 4, U = 4;
   constexpr bool LOG2 = sizeof(T) == 2 && HD >= 64;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * (256 / LPR) + threadIdx.x / LPR;
-  const int c = (threadIdx.x % LPR) * 4;
-  if (i >= rows) return;
-  if (ml[i].y == kDone) return;
-  float M = -INFINITY;
-  for (int s = 0; s < parts; ++s) M = fmaxf(M, ml[static_cast<int64_t>(s) * rows + i].x);
-  const float m0 = M == -INFINITY ? 0.f : M;
-  float L = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < parts; ++s) {
-    const int64_t at = static_cast<int64_t>(s) * rows + i;
-    const float2 p = ml[at];
-    if (p.y == 0.f) continue;
-    const float f = LOG2 ? __builtin_amdgcn_exp2f(p.x - m0) : expf(p.x - m0);
-    const float4 w = *reinterpret_cast<const float4*>(o + at * HD + c);
-    L = fmaf(p.y, f, L);
-    v[0] = fmaf(w.x, f, v[0]);
-    v[1] = fmaf(w.y, f, v[1]);
-    v[2] = fmaf(w.z, f, v[2]);
-    v[3] = fmaf(w.w, f, v[3]);
+  __shared__ float sv[256][4];
+  __shared__ float2 sml[256 / LPR];
+  const int group = threadIdx.x / LPR, lane = threadIdx.x % LPR, sub = group % per, c = 4 * lane;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * (256 / LPR / per) + group / per;
+  const bool live = i < rows && ml[i].y != kDone;
+  float M = -INFINITY, L = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (live) {
+    for (int s = sub + lane * per; s < parts; s += per * LPR) M = fmaxf(M, ml[static_cast<int64_t>(s) * rows + i].x);
+#pragma unroll
+    for (int off = 1; off < LPR; off <<= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+    const float m0 = M == -INFINITY ? 0.f : M;
+    for (int s0 = sub; s0 < parts; s0 += per * U) {
+      float2 p[U];
+      float4 w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = static_cast<int64_t>(min(s0 + u * per, parts - 1)) * rows + i;
+        p[u] = ml[at];
+        w[u] = *reinterpret_cast<const float4*>(o + at * HD + c);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (s0 + u * per >= parts || p[u].y == 0.f) continue;
+        const float f = LOG2 ? __builtin_amdgcn_exp2f(p[u].x - m0) : expf(p[u].x - m0);
+        L = fmaf(p[u].y, f, L);
+        v[0] = fmaf(w[u].x, f, v[0]);
+        v[1] = fmaf(w[u].y, f, v[1]);
+        v[2] = fmaf(w[u].z, f, v[2]);
+        v[3] = fmaf(w[u].w, f, v[3]);
+      }
+    }
   }
+  if (per > 1) {
+    if (lane == 0) sml[group] = make_float2(M, L);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sv[threadIdx.x][e] = v[e];
+    __syncthreads();
+    if (sub != 0) return;
+    for (int k = 0; k < per; ++k) M = fmaxf(M, sml[group + k].x);
+    const float m0 = M == -INFINITY ? 0.f : M;
+    L = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = 0.f;
+    for (int k = 0; k < per; ++k) {
+      const float2 p = sml[group + k];
+      if (p.y == 0.f) continue;
+      const float f = LOG2 ? __builtin_amdgcn_exp2f(p.x - m0) : expf(p.x - m0);
+      L = fmaf(p.y, f, L);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(sv[threadIdx.x + k * LPR][e], f, v[e]);
+    }
+  }
+  if (!live) return;
   const int t = static_cast<int>(i / H), h = static_cast<int>(i - static_cast<int64_t>(t) * H);
   const float inv = L == 0.f ? 0.f : 1.0f / L;
   T* op = out + t * out_stride + h * HD + c;
 #pragma unroll
   for (int e = 0; e < 4; ++e) op[e] = from_f32<T>(v[e] * inv);
-  if (c == 0 && lse != nullptr) lse[static_cast<int64_t>(h) * Trows + t] = L == 0.f ? -INFINITY : LOG2 ? (M + log2f(L)) * kLn2 : M + logf(L);
+  if (c == 0 && lse != nullptr)
+    lse[static_cast<int64_t>(h) * Trows + t] = L == 0.f ? -INFINITY : LOG2 ? (M + log2f(L)) * kLn2 : M + logf(L);
 }
 
 template <typename T>
-hipError_t f32_dispatch(hipStream_t s, const PagedAttention& a, dim3 g, int tiles) {
+hipError_t f32_dispatch(hipStream_t s, const PagedJobs& jobs, dim3 g) {
   const dim3 block(256);
-  switch (a.hd) {
-    case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16>, g, block, 0, s, a, tiles);
-    case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32>, g, block, 0, s, a, tiles);
+  switch (jobs.job[0].hd) {
+    case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16>, g, block, 0, s, jobs);
+    case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32>, g, block, 0, s, jobs);
     default: break;
   }
   if constexpr (sizeof(T) == 4) {
-    if (a.hd == 64) return launch(K_ATTENTION, paged_f32_kernel<T, 64>, g, block, 0, s, a, tiles);
-    if (a.hd == 128) return launch(K_ATTENTION, paged_f32_kernel<T, 128>, g, block, 0, s, a, tiles);
+    if (jobs.job[0].hd == 64) return launch(K_ATTENTION, paged_f32_kernel<T, 64>, g, block, 0, s, jobs);
+    if (jobs.job[0].hd == 128) return launch(K_ATTENTION, paged_f32_kernel<T, 128>, g, block, 0, s, jobs);
   }
   return hipErrorInvalidValue;
 }
@@ -1080,14 +1129,18 @@ hipError_t f32_dispatch(hipStream_t s, const PagedAttention& a, dim3 g, int tile
 template <typename T>
 hipError_t join_dispatch(hipStream_t s, const float2* ml, const float* o, int parts, int rows, int H, int T_,
                          int hd, void* out, int64_t os, float* lse) {
-  const int per = 256 / (hd / 4);
-  const dim3 g(static_cast<uint32_t>((rows + per - 1) / per)), block(256);
+  // groups of threads a row: until they number four a SIMD, or take few parts each
+  const int groups = 256 / (hd / 4);
+  int per = 1;
+  while (per < groups && 4 * per < parts && static_cast<int64_t>(rows) * per < 16 * device_cu_count()) per *= 2;
+  const int rpb = groups / per;
+  const dim3 g(static_cast<uint32_t>((rows + rpb - 1) / rpb)), block(256);
   T* op = static_cast<T*>(out);
   switch (hd) {
-    case 16: return launch(K_ATTENTION, paged_join_kernel<T, 16>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse);
-    case 32: return launch(K_ATTENTION, paged_join_kernel<T, 32>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse);
-    case 64: return launch(K_ATTENTION, paged_join_kernel<T, 64>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse);
-    case 128: return launch(K_ATTENTION, paged_join_kernel<T, 128>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse);
+    case 16: return launch(K_ATTENTION, paged_join_kernel<T, 16>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse, per);
+    case 32: return launch(K_ATTENTION, paged_join_kernel<T, 32>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse, per);
+    case 64: return launch(K_ATTENTION, paged_join_kernel<T, 64>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse, per);
+    case 128: return launch(K_ATTENTION, paged_join_kernel<T, 128>, g, block, 0, s, ml, o, parts, rows, H, T_, op, os, lse, per);
     default: return hipErrorInvalidValue;
   }
 }
@@ -1117,22 +1170,29 @@ int paged_chunk(bool many, int max_len, int64_t workgroups, int* splits) {
   return per * least;
 }
 
-hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention& a, bool many, int max_rows) {
+int64_t paged_blocks(const PagedAttention& a, bool many) {
   const int64_t pairs = static_cast<int64_t>(a.splits) * (a.H / a.G) * a.B;
+  return (many ? (pairs + 7) / 8 * 8 : pairs) * a.tiles;
+}
+
+hipError_t launch_paged_attention(hipStream_t s, int dtype, bool many, const PagedAttention* job, int jobs) {
+  if (jobs == 0) return hipSuccess;
+  PagedJobs w{};
+  w.job[0] = job[0];
+  w.job[1] = job[jobs - 1];
+  w.first = static_cast<uint32_t>(paged_blocks(job[0], many));
+  const dim3 g(w.first + (jobs > 1 ? static_cast<uint32_t>(paged_blocks(job[1], many)) : 0u));
+  const int hd = job[0].hd;
   if (many) {
-    const int tiles = (max_rows + kPagedManyRows - 1) / kPagedManyRows;
-    const dim3 g(static_cast<uint32_t>((pairs + 7) / 8 * 8 * tiles));
-    if (a.hd == 64) return launch(K_ATTENTION, paged_many_kernel<64, 2, 4>, g, dim3(256), 0, s, a, tiles, static_cast<int>(pairs));
-    return launch(K_ATTENTION, paged_many_kernel<128, 1, 8>, g, dim3(512), 0, s, a, tiles, static_cast<int>(pairs));
+    if (hd == 64) return launch(K_ATTENTION, paged_many_kernel<64, 2, 4>, g, dim3(256), 0, s, w);
+    return launch(K_ATTENTION, paged_many_kernel<128, 1, 8>, g, dim3(512), 0, s, w);
   }
-  const int tiles = (max_rows + 31) / 32;
-  const dim3 g(static_cast<uint32_t>(pairs * tiles));
-  if (paged_matrix(dtype, a.hd)) {
-    if (a.hd == 64) return launch(K_ATTENTION, paged_few_kernel<64>, g, dim3(256), 0, s, a, tiles);
-    return launch(K_ATTENTION, paged_few_kernel<128>, g, dim3(256), 0, s, a, tiles);
+  if (paged_matrix(dtype, hd)) {
+    if (hd == 64) return launch(K_ATTENTION, paged_few_kernel<64>, g, dim3(256), 0, s, w);
+    return launch(K_ATTENTION, paged_few_kernel<128>, g, dim3(256), 0, s, w);
   }
-  if (dtype == 1) return f32_dispatch<bf16_t>(s, a, g, tiles);
-  return f32_dispatch<float>(s, a, g, tiles);
+  if (dtype == 1) return f32_dispatch<bf16_t>(s, w, g);
+  return f32_dispatch<float>(s, w, g);
 }
 
 hipError_t launch_paged_join(hipStream_t s, int dtype, const float2* ml, const float* o, int parts, int T, int H,

@@ -447,7 +447,7 @@ struct PagedAppend {
 };
 hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a);
 
-// One launch's attention over the rows of `at`. The query rows of a sequence
+// Attention over the rows of `at`. The query rows of a sequence
 // that read one key/value head are taken together: packed row i of head g is
 // new row i / G, query head g G + i % G.
 struct PagedAttention {
@@ -460,6 +460,7 @@ struct PagedAttention {
   int T, B, H, G, hd;
   int causal;
   float scale;
+  int tiles;                  // blocks of packed rows of the longest sequence (kPagedManyRows each, or kPagedFewRows)
   int few_rows;               // a few-row launch takes the sequences of up to so many packed rows, a many-row one the others
   int chunk, splits;          // keys a split takes, a multiple of 128; splits
   int parts;                  // the call's parts from this launch's first on
@@ -470,12 +471,13 @@ struct PagedAttention {
   float2* ml;                 // [part][T * H] maximum and sum of the scores, or null: no row has parts
   float* o;                   // [part][T * H][hd] sums of values
 };
-constexpr int kPagedManyRows = 256;  // packed rows of the many-row kernel's workgroup
+constexpr int kPagedManyRows = 256, kPagedFewRows = 32;  // packed rows of a workgroup
 bool paged_matrix(int dtype, int hd);  // the bf16 matrix kernels take these heads: one for few rows, one for many
 // keys a split of up to max_len rows takes, and how many splits that makes
 int paged_chunk(bool many, int max_len, int64_t workgroups, int* splits);
-// max_rows: packed rows of the longest sequence of the launch
-hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention& a, bool many, int max_rows);
+int64_t paged_blocks(const PagedAttention& a, bool many);  // workgroups
+// one launch of up to two of them, of one type and kind
+hipError_t launch_paged_attention(hipStream_t s, int dtype, bool many, const PagedAttention* job, int jobs);
 hipError_t launch_paged_join(hipStream_t s, int dtype, const float2* ml, const float* o, int parts, int T, int H,
                              int hd, void* out, int64_t out_stride, float* lse);
 

@@ -85,29 +85,31 @@ size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
 // sequence goes to the few-row kernel.
 constexpr int kFewRows = 64;
 
-struct Launch {
+// The rows of one kind: the common prefix's, or the own ones of the sequences
+// of few packed rows, or of many.
+struct Part {
   bool many;
-  int max_rows;       // packed rows of its longest sequence; 0: nothing to launch
-  int chunk, splits;
+  int tiles;          // of the longest sequence
+  int chunk, splits;  // 0 splits: there are none
 };
 
-// What a call launches: over the common prefix, over the own rows of the
-// sequences of few packed rows, and of those of many. The parts of the prefix
-// come first, the others' after them, in the same places.
+// The parts of the prefix come first, the others' after them, in the same places.
 struct Plan {
-  Launch prefix, few, many;
+  Part prefix, few, many;
   int own() const { return std::max(few.splits, many.splits); }
   int parts() const { return prefix.splits + own(); }
-  // a launch finishes its rows itself where they have no other part
-  bool direct(const Launch& l) const { return prefix.splits == 0 && l.splits == 1; }
+  // rows are finished at once where they have no other part
+  bool direct(const Part& l) const { return prefix.splits == 0 && l.splits == 1; }
   bool join() const { return parts() > 1; }
 };
 
-Launch launch_of(bool many, int64_t max_rows, int64_t tiles, int max_len) {
-  Launch l{};
+int tile_of(bool many) { return many ? zsa::kPagedManyRows : zsa::kPagedFewRows; }
+
+Part part_of(bool many, int64_t max_rows, int64_t workgroups, int max_len) {
+  Part l{};
   l.many = many;
-  l.max_rows = static_cast<int>(max_rows);
-  l.chunk = zsa::paged_chunk(many, max_len, tiles, &l.splits);
+  l.tiles = static_cast<int>((max_rows + tile_of(many) - 1) / tile_of(many));
+  l.chunk = zsa::paged_chunk(many, max_len, workgroups, &l.splits);
   return l;
 }
 
@@ -118,16 +120,15 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   int64_t most[2] = {0, 0}, tiles[2] = {0, 0};
   for (int b = 0; b < batch; ++b) {
     const int64_t rows = (cu[b + 1] - cu[b]) * G;
-    const int many = matrix && rows > kFewRows, tile = many ? zsa::kPagedManyRows : 32;
+    const bool many = matrix && rows > kFewRows;
     most[many] = std::max(most[many], rows);
-    tiles[many] += (rows + tile - 1) / tile;
+    tiles[many] += (rows + tile_of(many) - 1) / tile_of(many);
   }
-  if (most[0] > 0) p.few = launch_of(false, most[0], tiles[0] * kv.n_kv_heads, max_len);
-  if (most[1] > 0) p.many = launch_of(true, most[1], tiles[1] * kv.n_kv_heads, max_len);
+  if (most[0] > 0) p.few = part_of(false, most[0], tiles[0] * kv.n_kv_heads, max_len);
+  if (most[1] > 0) p.many = part_of(true, most[1], tiles[1] * kv.n_kv_heads, max_len);
   if (prefix > 0) {
     const bool many = matrix && T * G > kFewRows;
-    const int tile = many ? zsa::kPagedManyRows : 32;
-    p.prefix = launch_of(many, T * G, (T * G + tile - 1) / tile * kv.n_kv_heads, prefix);
+    p.prefix = part_of(many, T * G, (T * G + tile_of(many) - 1) / tile_of(many) * kv.n_kv_heads, prefix);
   }
   return p;
 }
@@ -164,10 +165,6 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
   }
   if (T == 0) return ZSA_OK;
   const Plan p = plan_of(*kv, n_heads, batch, cu_host, max_kv_len, prefix_len);
-  for (const Launch* l : {&p.prefix, &p.few, &p.many})
-    if (static_cast<int64_t>(l->splits) * ((l->max_rows + 31) / 32) * kv->n_kv_heads * (l == &p.prefix ? 1 : batch) > (1 << 23))
-      return set_error(ZSA_EUNSUPPORTED, "%d sequences of up to %d rows of %d heads: more workgroups than a grid holds",
-                       batch, max_new, n_heads);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int64_t rows = static_cast<int64_t>(T) * n_heads;
   float2* ml = p.join() ? static_cast<float2*>(ws) : nullptr;
@@ -189,31 +186,40 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
   a.out = out;
   a.out_stride = out_stride;
   a.lse = lse;
-  auto go = [&](zsa::PagedAttention x, const Launch& l, int part, bool direct) {
-    x.few_rows = l.many ? (x.cu != nullptr ? kFewRows : 0) : (p.many.splits > 0 && x.cu != nullptr ? kFewRows : INT32_MAX);
-    x.chunk = l.chunk;
-    x.splits = l.splits;
-    x.parts = part == 0 && x.cu == nullptr ? l.splits : p.own();
-    x.direct = direct;
-    if (ml != nullptr) {
-      x.ml = ml + part * rows;
-      x.o = o + part * rows * kv->head_dim;
+  // the launches: of the few-row kernel and of the many-row one
+  zsa::PagedAttention job[2][2];
+  int jobs[2] = {0, 0};
+  for (const Part* l : {&p.prefix, &p.few, &p.many}) {
+    if (l->splits == 0) continue;
+    zsa::PagedAttention& x = job[l->many][jobs[l->many]++];
+    x = a;
+    const bool prefix = l == &p.prefix;
+    x.tiles = l->tiles;
+    x.chunk = l->chunk;
+    x.splits = l->splits;
+    x.few_rows = prefix ? (l->many ? 0 : INT32_MAX) : p.many.splits > 0 ? kFewRows : INT32_MAX;
+    x.parts = prefix ? l->splits : p.own();
+    x.direct = p.direct(*l);
+    if (prefix) {
+      x.at.table = prefix_pages;
+      x.at.max_pages = static_cast<int>((static_cast<int64_t>(prefix_len) + kv->page_size - 1) / kv->page_size);
+      x.cu = nullptr;
+      x.kv_len = nullptr;
+      x.max_len = prefix_len;
+      x.B = 1;
+      x.causal = 0;
+      x.direct = 0;
     }
-    return zsa::launch_paged_attention(s, kv->dtype, x, l.many, l.max_rows);
-  };
-  if (p.prefix.splits > 0) {
-    zsa::PagedAttention f = a;
-    f.at.table = prefix_pages;
-    f.at.max_pages = static_cast<int>((static_cast<int64_t>(prefix_len) + kv->page_size - 1) / kv->page_size);
-    f.cu = nullptr;
-    f.kv_len = nullptr;
-    f.max_len = prefix_len;
-    f.B = 1;
-    f.causal = 0;
-    HIP_TRY(go(f, p.prefix, 0, false), "prefix attention");
+    if (ml != nullptr) {
+      x.ml = ml + (prefix ? 0 : p.prefix.splits) * rows;
+      x.o = o + (prefix ? 0 : p.prefix.splits) * rows * kv->head_dim;
+    }
+    if (zsa::paged_blocks(x, l->many) > (1 << 22))
+      return set_error(ZSA_EUNSUPPORTED, "%d sequences of up to %d rows of %d heads: more workgroups than a grid holds",
+                       batch, max_new, n_heads);
   }
-  if (p.many.splits > 0) HIP_TRY(go(a, p.many, p.prefix.splits, p.direct(p.many)), "paged attention");
-  if (p.few.splits > 0) HIP_TRY(go(a, p.few, p.prefix.splits, p.direct(p.few)), "paged attention");
+  for (int many = 1; many >= 0; --many)
+    HIP_TRY(zsa::launch_paged_attention(s, kv->dtype, many != 0, job[many], jobs[many]), "paged attention");
   if (p.join())
     HIP_TRY(zsa::launch_paged_join(s, kv->dtype, ml, o, p.parts(), T, n_heads, kv->head_dim, out, out_stride, lse),
             "paged attention's parts");
@@ -268,9 +274,13 @@ int zsa_paged_append(void* stream, const zsa_paged_kv* kv, const void* k, int64_
   a.pos = pos;
   a.cu = cu_dev;
   a.kv_len = kv_len;
-  if (pos != nullptr)
-    for (int i = 0; i < kv->head_dim / 2; ++i)
-      a.inv_freq[i] = pow(static_cast<double>(rope_theta), -2.0 * i / kv->head_dim);
+  if (pos != nullptr) {
+    // theta^(-2i/hd) by repeated products: off by 63 roundings at most, 7e-15
+    // of an angle, which is 1e-9 rad at position 10^5; 64 powers take 2 us
+    const double step = pow(static_cast<double>(rope_theta), -2.0 / kv->head_dim);
+    a.inv_freq[0] = 1.0;
+    for (int i = 1; i < kv->head_dim / 2; ++i) a.inv_freq[i] = a.inv_freq[i - 1] * step;
+  }
   HIP_TRY(zsa::launch_paged_append(static_cast<hipStream_t>(stream), kv->dtype, a), "paged append");
   return ZSA_OK;
 }

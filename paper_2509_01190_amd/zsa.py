@@ -217,6 +217,12 @@ class Seqs:
             raise ValueError("cu_dev must hold the host's offsets as contiguous int32")
         return cls._of(host, cu_dev)
 
+    def host_ptr(self):
+        """The host offsets as the C entry points take them (made once per array)."""
+        if self.__dict__.get("_ptr_of") is not self.host:
+            self._ptr, self._ptr_of = _hp32(self.host), self.host
+        return self._ptr
+
     @property
     def lengths(self) -> List[int]:
         return [int(v) for v in np.diff(self.host)]
@@ -391,24 +397,44 @@ class PagedKV:
         self._ref = ctypes.byref(self._struct)
 
 
-def _paged_rows(kv: PagedKV, seqs: Seqs, kv_len: torch.Tensor, rows: torch.Tensor, what: str) -> int:
-    """Checks a call's rows against the cache; returns their stride."""
-    _require_cuda(rows, kv_len, seqs.dev)
+def _paged_rows(kv: PagedKV, seqs: Seqs, kv_len: torch.Tensor) -> None:
+    """Checks a call's sequences against the cache."""
+    dev = kv.pool.device
     if seqs.batch != kv.table.shape[0]:
         raise ValueError(f"{seqs.batch} sequences, {kv.table.shape[0]} rows of the table")
-    if kv_len.dtype != torch.int32 or kv_len.numel() != seqs.batch or not kv_len.is_contiguous():
-        raise ValueError("kv_len must be contiguous int32, one a sequence")
-    return _rows_stride(kv, seqs, rows, what)
+    if (kv_len.dtype != torch.int32 or kv_len.numel() != seqs.batch or not kv_len.is_contiguous()
+            or kv_len.device != dev or seqs.dev.device != dev):
+        raise ValueError("kv_len must be contiguous int32, one a sequence, and on the cache's device as the offsets")
 
 
-def _rows_stride(kv: PagedKV, seqs: Seqs, rows: torch.Tensor, what: str) -> int:
-    if rows.dim() != 2 or rows.shape[0] != seqs.total:
-        raise ValueError(f"{what} must have {seqs.total} rows")
+def _rows_stride(kv: PagedKV, rows: torch.Tensor, total: int, cols: int, what: str) -> int:
+    """The stride of a call's rows [total, cols], checked against the cache."""
+    if rows.dim() != 2 or tuple(rows.shape) != (total, cols):
+        raise ValueError(f"{what} must have {total} rows of {cols} columns")
     if rows.dtype != kv.pool.dtype or rows.device != kv.pool.device:
         raise ValueError(f"{what} must have the cache's type and device")
-    if rows.numel() > 0 and rows.stride(1) != 1:
+    stride, step = rows.stride()
+    if step != 1 and cols > 1 and total > 0:
         raise ValueError(f"{what}'s columns must be contiguous")
-    return rows.stride(0) if rows.shape[0] > 1 else rows.shape[1]
+    return stride if total > 1 else cols
+
+
+class _On:
+    """The device of a call made current for it, and its stream. Cheaper than
+    torch.cuda.device where it is current already, as it mostly is."""
+
+    def __init__(self, dev: torch.device):
+        self.dev, self.was = dev, None
+
+    def __enter__(self) -> int:
+        if torch.cuda.current_device() != self.dev.index:
+            self.was = torch.cuda.device(self.dev)
+            self.was.__enter__()
+        return torch._C._cuda_getCurrentRawStream(self.dev.index)
+
+    def __exit__(self, *e):
+        if self.was is not None:
+            self.was.__exit__(*e)
 
 
 def paged_append(kv: PagedKV, k: torch.Tensor, v: torch.Tensor, seqs: Seqs, kv_len: torch.Tensor,
@@ -419,28 +445,25 @@ def paged_append(kv: PagedKV, k: torch.Tensor, v: torch.Tensor, seqs: Seqs, kv_l
     sequence's rows with the new ones, which are the last. With ``pos`` [T]
     int32 the keys are rotated on the way, and so are the queries ``q``
     [T, n_heads * hd] if given, which are returned."""
-    ks = _paged_rows(kv, seqs, kv_len, k, "k")
-    vs = _rows_stride(kv, seqs, v, "v")
+    _paged_rows(kv, seqs, kv_len)
+    T, dev = seqs.total, kv.pool.device
     kvd = kv.n_kv_heads * kv.head_dim
-    if k.shape[1] != kvd or v.shape[1] != kvd:
-        raise ValueError(f"k and v must have {kvd} columns")
-    if pos is not None:
-        _require_cuda(pos)
-        if pos.dtype != torch.int32 or pos.numel() != seqs.total or not pos.is_contiguous():
-            raise ValueError("pos must be contiguous int32, one a row")
+    ks, vs = _rows_stride(kv, k, T, kvd, "k"), _rows_stride(kv, v, T, kvd, "v")
+    if pos is not None and (pos.dtype != torch.int32 or pos.numel() != T or not pos.is_contiguous()
+                            or pos.device != dev):
+        raise ValueError("pos must be contiguous int32, one a row, on the cache's device")
     out, qs, qos = None, 0, 0
     if q is not None:
-        qs = _rows_stride(kv, seqs, q, "q")
-        if n_heads < 1 or q.shape[1] != n_heads * kv.head_dim:
-            raise ValueError(f"q must have {n_heads} heads of {kv.head_dim}")
-        out = torch.empty((seqs.total, q.shape[1]), dtype=q.dtype, device=q.device)
-        qos = q.shape[1]
-    if seqs.total == 0:
+        qos = n_heads * kv.head_dim
+        qs = _rows_stride(kv, q, T, qos, "q")
+        out = q.new_empty((T, qos))
+    if T == 0:
         return out
-    with torch.cuda.device(k.device):
+    with _On(dev) as stream:
         _check(lib().zsa_paged_append(
-            _stream(k.device), kv._ref, _p(k), ks, _p(v), vs, _p(q), qs, n_heads, _p(out), qos, _p(pos),
-            rope_theta, seqs.batch, _hp32(seqs.host), _p(seqs.dev), _p(kv_len)))
+            stream, kv._ref, k.data_ptr(), ks, v.data_ptr(), vs, None if q is None else q.data_ptr(), qs, n_heads,
+            None if q is None else out.data_ptr(), qos, None if pos is None else pos.data_ptr(), rope_theta,
+            seqs.batch, seqs.host_ptr(), seqs.dev.data_ptr(), kv_len.data_ptr()))
     return out
 
 
@@ -451,32 +474,30 @@ def prefix_attention(q: torch.Tensor, kv: PagedKV, n_heads: int, seqs: Seqs, kv_
     """paged_attention for sequences that share their first ``prefix_len``
     rows, which lie in the pages ``prefix_pages`` (int32, on the device)
     and come before the rows that kv_len counts. Returns (out, lse or None)."""
-    qs = _paged_rows(kv, seqs, kv_len, q, "q")
-    hd, size = kv.head_dim, kv.pool.shape[1]
-    if q.shape[1] != n_heads * hd:
-        raise ValueError(f"q must have {n_heads} heads of {hd}")
+    _paged_rows(kv, seqs, kv_len)
+    hd, size, T, dev = kv.head_dim, kv.pool.shape[1], seqs.total, kv.pool.device
+    width = n_heads * hd
+    qs = _rows_stride(kv, q, T, width, "q")
     if prefix_len > 0:
-        if prefix_pages is None:
-            raise ValueError("prefix_pages is missing")
-        _require_cuda(prefix_pages)
-        if (prefix_pages.dtype != torch.int32 or not prefix_pages.is_contiguous()
-                or prefix_pages.numel() * size < prefix_len or prefix_pages.device != q.device):
-            raise ValueError("prefix_pages must be contiguous int32 ids of pages that hold prefix_len rows")
+        if (prefix_pages is None or prefix_pages.dtype != torch.int32 or not prefix_pages.is_contiguous()
+                or prefix_pages.numel() * size < prefix_len or prefix_pages.device != dev):
+            raise ValueError("prefix_pages must be contiguous int32 ids, on the cache's device, of pages that hold "
+                             "prefix_len rows")
     if max_kv_len is None:
         max_kv_len = kv.table.shape[1] * size
     if scale is None:
-        scale = 1.0 / float(np.sqrt(hd))
-    T = seqs.total
-    out = torch.empty((T, n_heads * hd), dtype=q.dtype, device=q.device)
-    lse = torch.empty((n_heads, T), dtype=torch.float32, device=q.device) if want_lse else None
-    cu = _hp32(seqs.host)
-    with torch.cuda.device(q.device):
-        wsz = lib().zsa_paged_attention_workspace_size(kv._ref, n_heads, seqs.batch, cu, max_kv_len, prefix_len)
-        ws = torch.empty(wsz, dtype=torch.uint8, device=q.device) if wsz else None
-        _check(lib().zsa_prefix_attention(
-            _stream(q.device), kv._ref, _p(q), qs, n_heads, int(causal), scale, seqs.batch, cu,
-            _p(seqs.dev), _p(kv_len), max_kv_len, _p(prefix_pages), prefix_len, _p(out), n_heads * hd,
-            _p(lse), _p(ws), wsz))
+        scale = hd ** -0.5
+    out = q.new_empty((T, width))
+    lse = q.new_empty((n_heads, T), dtype=torch.float32) if want_lse else None
+    cu, l = seqs.host_ptr(), lib()
+    with _On(dev) as stream:
+        wsz = l.zsa_paged_attention_workspace_size(kv._ref, n_heads, seqs.batch, cu, max_kv_len, prefix_len)
+        ws = q.new_empty(wsz, dtype=torch.uint8) if wsz else None
+        _check(l.zsa_prefix_attention(
+            stream, kv._ref, q.data_ptr(), qs, n_heads, int(causal), scale, seqs.batch, cu, seqs.dev.data_ptr(),
+            kv_len.data_ptr(), max_kv_len, None if prefix_pages is None else prefix_pages.data_ptr(), prefix_len,
+            out.data_ptr(), width, None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
+            wsz))
     return out, lse
 
 
