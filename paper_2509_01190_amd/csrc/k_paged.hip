@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
   __shared__ __align__(1024) unsigned char smem[SBYTES];
   __shared__ float sm[NW][32], sl[NW][32];
   const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
-  const PagedAttention& a = jobs.job[which];
+  const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
   const int split = block % a.splits, it0 = block / a.splits;
   const int tile = it0 % a.tiles, gb = it0 / a.tiles, Hkv = a.H / a.G, g = gb % Hkv, b = gb / Hkv;
   const Span sp = span_of(a, b);
@@ -451,7 +451,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // the row blocks of a pair (split of the keys, key/value head, sequence) run
   // on one XCD one after another, the last ones, which see most keys, first
   const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
-  const PagedAttention& a = jobs.job[which];
+  const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
   const int Hkv = a.H / a.G, pair = (block >> 3) / a.tiles * 8 + (block & 7);
   if (pair >= a.splits * Hkv * a.B) return;
   const int tile = a.tiles - 1 - (block >> 3) % a.tiles;
@@ -866,7 +866,7 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedJobs jobs) {
   __shared__ float so[NW][HD * HP];
   __shared__ float sm[NW][32], sl[NW][32];
   const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
-  const PagedAttention& a = jobs.job[which];
+  const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
   const int split = block % a.splits, it0 = block / a.splits;
   const int tile = it0 % a.tiles, gb = it0 / a.tiles, g = gb % (a.H / a.G), b = gb / (a.H / a.G);
   const Span sp = span_of(a, b);
