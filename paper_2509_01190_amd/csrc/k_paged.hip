@@ -163,6 +163,11 @@ __device__ __forceinline__ scalar_ids scalar(const int32_t* p) {
   return reinterpret_cast<scalar_ids>(reinterpret_cast<uintptr_t>(p));
 }
 
+// Workgroups of the few-row kernels: the (key/value head, sequence) pairs
+// vary fastest, then the blocks of rows, then the splits. Workgroup L runs on
+// XCD L % 8: with the splits fastest and 2, 4 or 8 of them a ragged batch's
+// last splits, mostly empty, were all on the same XCDs.
+
 // bf16, heads of 64 and 128, up to 32 packed rows at a time: bound by the
 // cached rows' bytes. A workgroup takes 32 packed rows of one (sequence,
 // key/value head) and a split of its keys; its four waves take 32-key tiles in
@@ -186,8 +191,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
   __shared__ float sm[NW][32], sl[NW][32];
   const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
   const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
-  const int split = block % a.splits, it0 = block / a.splits;
-  const int tile = it0 % a.tiles, gb = it0 / a.tiles, Hkv = a.H / a.G, g = gb % Hkv, b = gb / Hkv;
+  const int Hkv = a.H / a.G, pair = block % (Hkv * a.B), st = block / (Hkv * a.B);
+  const int g = pair % Hkv, b = pair / Hkv, tile = st % a.tiles, split = st / a.tiles;
   const Span sp = span_of(a, b);
   const int i0 = tile * 32;
   if (i0 >= sp.rows || sp.rows > a.few_rows) return;
@@ -455,7 +460,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int Hkv = a.H / a.G, pair = (block >> 3) / a.tiles * 8 + (block & 7);
   if (pair >= a.splits * Hkv * a.B) return;
   const int tile = a.tiles - 1 - (block >> 3) % a.tiles;
-  const int split = pair / Hkv % a.splits, g = pair % Hkv, b = pair / Hkv / a.splits;
+  const int split = pair / (Hkv * a.B), g = pair % Hkv, b = pair / Hkv % a.B;
   const Span sp = span_of(a, b);
   const int i0 = tile * BQ;
   if (i0 >= sp.rows || sp.rows <= a.few_rows) return;
@@ -867,8 +872,8 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedJobs jobs) {
   __shared__ float sm[NW][32], sl[NW][32];
   const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
   const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
-  const int split = block % a.splits, it0 = block / a.splits;
-  const int tile = it0 % a.tiles, gb = it0 / a.tiles, g = gb % (a.H / a.G), b = gb / (a.H / a.G);
+  const int Hkv = a.H / a.G, pair = block % (Hkv * a.B), st = block / (Hkv * a.B);
+  const int g = pair % Hkv, b = pair / Hkv, tile = st % a.tiles, split = st / a.tiles;
   const Span sp = span_of(a, b);
   const int i0 = tile * 32;
   if (i0 >= sp.rows) return;
@@ -1159,10 +1164,11 @@ hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a) {
 bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 64; }
 
 // Splits of the keys. The few-row kernels: enough workgroups for four a CU, of
-// 128 keys at least. The many-row kernel: two a CU, of 512 keys at least (a
+// 512 keys at least: a second split needs the parts joined, which takes as long
+// (4 sequences of up to 300 rows, 12 heads of 64: 10.9 us, in splits of 128 14.9). The many-row kernel: two a CU, of 512 keys at least (a
 // split's part is as many bytes as 256 of its keys).
 int paged_chunk(bool many, int max_len, int64_t workgroups, int* splits) {
-  const int least = many ? 512 : 128;
+  const int least = 512;
   const int64_t blocks = std::max(1, (max_len + least - 1) / least), wgs = std::max<int64_t>(workgroups, 1);
   const int64_t want = std::min(blocks, std::max<int64_t>(1, ((many ? 2 : 4) * static_cast<int64_t>(device_cu_count()) + wgs - 1) / wgs));
   const int per = static_cast<int>((blocks + want - 1) / want);

@@ -83,7 +83,7 @@ size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
 
 // Packed rows (new rows times query heads per key/value head) up to which a
 // sequence goes to the few-row kernel.
-constexpr int kFewRows = 64;
+constexpr int kFewRows = 32;
 
 // The rows of one kind: the common prefix's, or the own ones of the sequences
 // of few packed rows, or of many.
