@@ -144,7 +144,7 @@ __device__ __forceinline__ Span span_of(const PagedAttention& a, int b) {
 // one kind. The prefix's workgroups, which have more to do, come first.
 struct PagedJobs {
   PagedAttention job[2];
-  uint32_t first;  // workgroups of the first
+  uint32_t first, blocks;  // workgroups of the first, and of both
 };
 
 // The parts of a row: (maximum, sum) in ml and the sums of values in o, one of
@@ -180,29 +180,35 @@ __device__ __forceinline__ scalar_ids scalar(const int32_t* p) {
 // one row, which are the operand of the second product (k_attn.hip). P meets V
 // as two bf16 numbers whose sum has 16 bits: the matrix cores have the time.
 template <int HD>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2))) void paged_few_kernel(
-    PagedJobs jobs) {
-  constexpr int NW = 4, KK = HD / 16, CT = HD / 32, CPR = HD / 8;
+struct FewShared {  // LDS of a group of four waves
+  static constexpr int NW = 4, HP = 33;  // merge row stride: [channel][row]
+  static constexpr int TILES = NW * 64 * HD * 2, MERGE = NW * HD * HP * 4;
+  unsigned char tiles[MERGE > TILES ? MERGE : TILES];
+  float m[NW][32], l[NW][32];
+};
+
+// the work of one of `blocks` groups of four waves, as its thread `tid`; all threads of the workgroup call it
+template <int HD>
+__device__ __forceinline__ void few_rows(const PagedAttention& a, int block, bool there, int tid, FewShared<HD>& shared) {
+  constexpr int NW = FewShared<HD>::NW, KK = HD / 16, CT = HD / 32, CPR = HD / 8;
   constexpr int RB = HD * 2, HALF = 32 * RB;    // a tile of 32 rows of K, or V
   constexpr int RPL = 1024 / RB, NL = 16 / RPL;  // rows a load, loads per 16 rows
-  constexpr int HP = 33;                         // merge row stride: [channel][row]
-  constexpr int SBYTES = NW * HD * HP * 4 > NW * 2 * HALF ? NW * HD * HP * 4 : NW * 2 * HALF;
-  __shared__ __align__(1024) unsigned char smem[SBYTES];
-  __shared__ float sm[NW][32], sl[NW][32];
-  const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
-  const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
+  constexpr int HP = FewShared<HD>::HP;
+  unsigned char* smem = shared.tiles;
+  auto& sm = shared.m;
+  auto& sl = shared.l;
   const int Hkv = a.H / a.G, pair = block % (Hkv * a.B), st = block / (Hkv * a.B);
   const int g = pair % Hkv, b = pair / Hkv, tile = st % a.tiles, split = st / a.tiles;
   const Span sp = span_of(a, b);
   const int i0 = tile * 32;
-  if (i0 >= sp.rows || sp.rows > a.few_rows) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool live = there && i0 < sp.rows && sp.rows <= a.few_rows;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int row = min(i0 + l32, sp.rows - 1);  // rows past the sequence are not stored
   const int lim = a.causal ? min(sp.first + row / a.G, sp.len) : sp.len;
   const int lim0 = a.causal ? min(sp.first + i0 / a.G, sp.len) : sp.len;  // the tile's first row's
   const int last = a.causal ? min(sp.first + min(i0 + 31, sp.rows - 1) / a.G, sp.len) : sp.len;
-  const int k0 = split * a.chunk, kend = min(last, k0 + a.chunk);
+  const int k0 = split * a.chunk, kend = live ? min(last, k0 + a.chunk) : 0;
   const float scale_log2 = a.scale * kLog2e;
 
   // K row r of a tile keeps its 16-byte chunk c at c ^ ksw(r), V row r at c ^ vsw(r) (k_attn.hip)
@@ -261,7 +267,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
     load(j0, pg0, pg1, lds0 + HALF, vcol, voff);
   }
   bf16x8_t qf[KK];
-  {
+  if (j0 < kend) {
     const bf16_t* qp = static_cast<const bf16_t*>(a.q) + static_cast<int64_t>(sp.lo + row / a.G) * a.q_stride +
                        (g * a.G + row % a.G) * HD;
 #pragma unroll
@@ -382,7 +388,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
     sm[wave][l32] = m_run == -INFINITY ? -INFINITY : m_run * scale_log2;
     sl[wave][l32] = l_run;
   }
-  const int nr = min(32, sp.rows - i0);
+  const int nr = live ? min(32, sp.rows - i0) : 0;
   if (l32 < nr) {
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
@@ -426,6 +432,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
   }
 }
 
+template <int HD>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2))) void paged_few_kernel(
+    PagedJobs jobs) {
+  __shared__ __align__(1024) FewShared<HD> shared;
+  const int which = blockIdx.x >= jobs.first;
+  const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
+  few_rows<HD>(a, blockIdx.x - (which ? jobs.first : 0), true, threadIdx.x, shared);
+}
+
 // bf16, heads of 64 and 128, many packed rows: bound by the products. A
 // workgroup takes 32 QB NW packed rows of one (sequence, key/value head) and a
 // split of its keys; all waves share the K and V tiles of 64 keys, three of
@@ -443,20 +458,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 
 //  * The packed rows put the G query heads that share a key/value head into
 //    one workgroup: its tiles are read once for all of them.
 template <int HD, int QB, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_many_kernel(
-    PagedJobs jobs) {
+struct ManyShared {
+  static constexpr int WQ = 32 * QB, BUF = 2 * 64 * HD * 2, NB = 3, OLD = HD + 8;
+  unsigned char tiles[NB * BUF > NW * WQ * OLD * 2 ? NB * BUF : NW * WQ * OLD * 2];
+};
+
+template <int HD, int QB, int NW>
+__device__ __forceinline__ void many_rows(const PagedAttention& a, int block, ManyShared<HD, QB, NW>& shared) {
   constexpr int WQ = 32 * QB, BQ = WQ * NW, BK = 64;
   constexpr int KK = HD / 16, CT = HD / 32, CPR = HD / 8;
-  constexpr int RB = HD * 2, HALF = BK * RB, BUF = 2 * HALF, NB = 3, OLD = HD + 8;
-  constexpr int SBYTES = NB * BUF > NW * WQ * OLD * 2 ? NB * BUF : NW * WQ * OLD * 2;
+  constexpr int RB = HD * 2, HALF = BK * RB, BUF = 2 * HALF, OLD = HD + 8;
   constexpr int RPL = 1024 / RB, LPW = HALF / 1024 / NW;  // rows per load, loads per wave and operand
-  static_assert(LPW * NW * 1024 == HALF && NW * RPL % 16 == 0, "tile split");
-  __shared__ __align__(1024) unsigned char smem[SBYTES];
+  static_assert(LPW * NW * 1024 == HALF && NW * RPL % 16 == 0 && BQ == kPagedManyRows, "tile split");
+  unsigned char* smem = shared.tiles;
 
-  // the row blocks of a pair (split of the keys, key/value head, sequence) run
+  // the row blocks of a pair (key/value head, sequence, split of the keys) run
   // on one XCD one after another, the last ones, which see most keys, first
-  const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
-  const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
   const int Hkv = a.H / a.G, pair = (block >> 3) / a.tiles * 8 + (block & 7);
   if (pair >= a.splits * Hkv * a.B) return;
   const int tile = a.tiles - 1 - (block >> 3) % a.tiles;
@@ -857,19 +874,54 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
-// fp32 storage, and bf16 at head dims 16 and 32: both products on
-// v_mfma_f32_32x32x2_f32, fp32 operands and sums (the layout is that of the
-// fp32 attention over packed rows, k_attn.hip). One workgroup of four waves
-// per (split of the keys, 32 packed rows, key/value head, sequence); the waves
-// take the split's 32-key tiles in turn and their (max, sum, O) are merged
-// through LDS in wave order.
+// The many-row kernel, and the few-row one's work in the same launch: its
+// workgroups fill the CUs that the first, longer ones leave.
+template <int HD, int QB, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_many_kernel(PagedJobs many,
+                                                                                                      PagedJobs few) {
+  constexpr int GROUPS = NW / FewShared<HD>::NW;
+  __shared__ __align__(1024) union {
+    ManyShared<HD, QB, NW> many;
+    FewShared<HD> few[GROUPS];
+  } shared;
+  if (blockIdx.x < many.blocks) {
+    const int which = blockIdx.x >= many.first;
+    const PagedAttention a = many.job[which];  // (a copy: what it holds stays in registers)
+    many_rows<HD, QB, NW>(a, blockIdx.x - (which ? many.first : 0), shared.many);
+  } else {
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+    const uint32_t block = (blockIdx.x - many.blocks) * GROUPS + group;
+    const int which = block >= few.first;
+    const PagedAttention a = few.job[which];
+    few_rows<HD>(a, block - (which ? few.first : 0), block < few.blocks, threadIdx.x & 255, shared.few[group]);
+  }
+}
+
+// fp32 storage, and bf16 at head dims 16 and 32: the few-row kernel with both
+// products on v_mfma_f32_32x32x2_f32, fp32 operands and sums, for any number of
+// packed rows, 32 at a time. K is read from LDS 16 bytes a lane, as the first
+// operand has it; V one number a lane, 32 consecutive channels a half-wave. The
+// exponentials are expf (the fp32 attention in k_attn.hip says why).
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void paged_f32_kernel(PagedJobs jobs) {
-  constexpr int NW = 4, KK = HD / 8;
+struct F32Shared {
+  static constexpr int NW = 4, HP = 33;  // merge row stride: [channel][row]
+  static constexpr int TILES = NW * 64 * HD * sizeof(T), MERGE = NW * HD * HP * 4;
+  unsigned char tiles[MERGE > TILES ? MERGE : TILES];
+  float m[NW][32], l[NW][32];
+};
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 1 : HD == 64 ? 2 : 3))) void paged_f32_kernel(
+    PagedJobs jobs) {
+  constexpr int NW = 4, E = sizeof(T), KK = HD / 8;
   constexpr int CT = HD < 32 ? 1 : HD / 32;  // 32-channel blocks of O (half empty at HD 16)
-  constexpr int HP = 33;                     // merge row stride: [channel][query]
-  __shared__ float so[NW][HD * HP];
-  __shared__ float sm[NW][32], sl[NW][32];
+  constexpr int RB = HD * E, HALF = 32 * RB, CPR = RB / 16;
+  constexpr int RPL = 1024 / RB < 16 ? 1024 / RB : 16, NL = 16 / RPL;  // rows a load, loads per 16 rows
+  constexpr int HP = F32Shared<T, HD>::HP;
+  __shared__ __align__(1024) F32Shared<T, HD> shared;
+  unsigned char* smem = shared.tiles;
+  auto& sm = shared.m;
+  auto& sl = shared.l;
   const int which = blockIdx.x >= jobs.first, block = blockIdx.x - (which ? jobs.first : 0);
   const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
   const int Hkv = a.H / a.G, pair = block % (Hkv * a.B), st = block / (Hkv * a.B);
@@ -877,61 +929,98 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedJobs jobs) {
   const Span sp = span_of(a, b);
   const int i0 = tile * 32;
   if (i0 >= sp.rows) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int row = min(i0 + l32, sp.rows - 1);  // rows past the sequence are not stored
   const int lim = a.causal ? min(sp.first + row / a.G, sp.len) : sp.len;
   const int lim0 = a.causal ? min(sp.first + i0 / a.G, sp.len) : sp.len;  // the tile's first row's
   const int last = a.causal ? min(sp.first + min(i0 + 31, sp.rows - 1) / a.G, sp.len) : sp.len;
   const int k0 = split * a.chunk, kend = min(last, k0 + a.chunk);
-  const int rs = 2 * a.at.kvd;
-  const T* pool = static_cast<const T*>(a.at.pool);
-  const T* qp = static_cast<const T*>(a.q) + static_cast<int64_t>(sp.lo + row / a.G) * a.q_stride + (g * a.G + row % a.G) * HD;
-  const bool vch = HD >= 32 || l32 < HD;  // lanes whose channel exists
-  float4 qf[KK];
+
+  // K row r of a tile keeps its 16-byte chunk c at c ^ ksw(r): the rows of a
+  // read phase fall on all banks; V row r at c ^ vsw(r): rows four apart, which
+  // the two half-waves read at once, do
+  auto ksw = [](int r) { return CPR >= 16 ? r & 15 : CPR == 8 ? (r >> 1) & 7 : CPR == 4 ? (r >> 2) & 3 : (r >> 3) & 1; };
+  auto vsw = [](int r) { return CPR >= 16 ? ((r >> 2) & 1) << 3 : 0; };
+  const uint32_t rowb = static_cast<uint32_t>(a.at.kvd) * (2 * E);
+  uint32_t koff[NL], voff[NL];
 #pragma unroll
-  for (int s = 0; s < KK; ++s) qf[s] = load4<T>(qp + 8 * s + 4 * half);
+  for (int i = 0; i < NL; ++i) {
+    const int r = i * RPL + lane / CPR;
+    koff[i] = r * rowb + (((lane % CPR) ^ ksw(r)) << 4);
+    voff[i] = r * rowb + (((lane % CPR) ^ vsw(r)) << 4);
+  }
+  unsigned char* mine = smem + wave * (2 * HALF);
+  const uint32_t lds0 = lds_address(smem) + wave * (2 * HALF);
+  const scalar_ids table = scalar(sp.table);
+  const char* pool = static_cast<const char*>(a.at.pool);
+  // 16 rows from row j on, of page `page` (-1 where the sequence has ended): `col` bytes into a row
+  auto resource = [&](int j, int page, uint32_t col) {
+    const bool there = page >= 0 && page < a.at.n_pages;
+    const uint32_t bytes = there ? static_cast<uint32_t>(min(sp.len - j, 16)) * rowb - col : 0u;
+    u32x4 res = buffer_resource(pool + (there ? page : 0) * (a.at.page_stride * E) +
+                                    static_cast<uint32_t>(j & ((1 << a.at.shift) - 1)) * rowb + col,
+                                bytes);
+    // a load in asm may follow a vector instruction's write of its scalar operands by five states at least
+    asm volatile("s_nop 4" : "+s"(res));
+    return res;
+  };
+  auto page_of = [&](int j) { return j < sp.len ? table[j >> a.at.shift] : -1; };
+  const uint32_t kcol = g * RB, vcol = rowb / 2 + g * RB;
+  auto load = [&](int j0, int pg0, int pg1, uint32_t lds, uint32_t col, const uint32_t (&off)[NL]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 res = resource(j0 + 16 * h, h == 0 ? pg0 : pg1, col);
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        if (RPL * CPR == 64 || lane < RPL * CPR) lds_load16(lds + (h * NL + i) * (RPL * RB), off[i], res);
+    }
+  };
+
   float m_run = -INFINITY, l_run = 0.f;  // of the scaled scores; l_run: this lane's keys only
   f32x16_t o[CT];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
-  for (int j0 = k0 + wave * 32; j0 < kend; j0 += 32 * NW) {
-    // a page holds 16 rows at least: two of them here
-    const T* base[2];
-    bool there[2];
+  const bool vch = HD >= 32 || l32 < HD;  // lanes whose channel exists
+  const int ks0 = ksw(l32);
+  int j0 = k0 + wave * 32;
+  int pg0 = page_of(j0), pg1 = page_of(j0 + 16);
+  if (j0 < kend) {
+    load(j0, pg0, pg1, lds0, kcol, koff);
+    load(j0, pg0, pg1, lds0 + HALF, vcol, voff);
+  }
+  float4 qf[KK];
+  if (j0 < kend) {
+    const T* qp = static_cast<const T*>(a.q) + static_cast<int64_t>(sp.lo + row / a.G) * a.q_stride + (g * a.G + row % a.G) * HD;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int j = j0 + 16 * i;
-      const int page = j < sp.len ? sp.table[j >> a.at.shift] : -1;
-      there[i] = page >= 0 && page < a.at.n_pages;
-      base[i] = pool + (there[i] ? page : 0) * a.at.page_stride +
-                static_cast<int64_t>(j & ((1 << a.at.shift) - 1)) * rs + g * HD;
-    }
-    float vr[CT][16];
+    for (int s = 0; s < KK; ++s) qf[s] = load4<T>(qp + 8 * s + 4 * half);
+    // here before the loop, which would otherwise wait for every load in it
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      // rows past the sequence count as zeros (their probability is 0)
-      const int jj = 8 * (r >> 2) + 4 * half + (r & 3), i = r >> 3;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-        vr[ct][r] = there[i] && j0 + jj < sp.len && vch
-                        ? to_f32(base[i][(jj & 15) * rs + a.at.kvd + ct * 32 + (HD < 32 ? l32 % HD : l32)])
-                        : 0.f;
-    }
+    for (int s = 0; s < KK; ++s) asm volatile("" : "+v"(qf[s].x), "+v"(qf[s].y), "+v"(qf[s].z), "+v"(qf[s].w));
+  }
+  for (; j0 < kend; j0 += 32 * NW) {
+    const int jn = j0 + 32 * NW;
+    const bool more = jn < kend;
+    pg0 = page_of(jn);
+    pg1 = page_of(jn + 16);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // K is here, V may be under way
+    __builtin_amdgcn_sched_barrier(0);
     f32x16_t s = {};
-    const bool kin = there[l32 >> 4] && j0 + l32 < sp.len;
-    const T* kp = (l32 >> 4 ? base[1] : base[0]) + (l32 & 15) * rs + 4 * half;
 #pragma unroll
     for (int t = 0; t < KK; ++t) {
-      const float4 k4 = kin ? load4<T>(kp + 8 * t) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const int ch = (8 * t + 4 * half) * E;  // byte of the lane's four channels in a row
+      const float4 k4 = load4<T>(reinterpret_cast<const T*>(mine + l32 * RB + (((ch >> 4) ^ ks0) << 4) + (ch & 15)));
       s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, qf[t].x, s, 0, 0, 0);
       s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, qf[t].y, s, 0, 0, 0);
       s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.z, qf[t].z, s, 0, 0, 0);
       s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.w, qf[t].w, s, 0, 0, 0);
     }
-    // s[r]: key j0 + 8 (r/4) + 4 half + r%4, query row
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) load(jn, pg0, pg1, lds0, kcol, koff);
+    // s[r]: key j0 + 8 (r/4) + 4 half + r%4, packed row `row`
     const bool edge = j0 + 32 > lim0;
     float mloc = -INFINITY;
 #pragma unroll
@@ -957,70 +1046,91 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PagedJobs jobs) {
       s[r] = expf(s[r] - m_use);
       l_run += s[r];
     }
-    // A masked key's V row must not reach a query that does not see it, also
-    // where it holds an infinity or a NaN, which a product with its zero
-    // probability would spread. Such rows are rare: the tile then goes
-    // through the vector ALU, key by key.
+    if (more)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // V is here, the next K may be under way
+    else
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    // hidden keys' values that are not finite: key by key (few_rows)
     bool odd = false;
-    if (edge) {
+    if (lim0 < min(j0 + 32, sp.len)) {
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
+      for (int i = 0; i < HALF / 1024; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(mine + HALF + i * 1024 + lane * 16);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) odd |= !(fabsf(vr[ct][r]) <= 3.402823466e38f);
+        for (int e = 0; e < 4; ++e)
+          odd |= (w[e] & 0x7f800000u) == 0x7f800000u || (E == 2 && (w[e] & 0x7f80u) == 0x7f80u);
+      }
       odd = __builtin_amdgcn_ballot_w64(odd) != 0;
     }
     if (!odd) {
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
+      for (int r = 0; r < 16; ++r) {
+        const int jj = 8 * (r >> 2) + 4 * half + (r & 3);
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          o[ct] = __builtin_amdgcn_mfma_f32_32x32x2f32(vr[ct][r], s[r], o[ct], 0, 0, 0);
+        for (int ct = 0; ct < CT; ++ct) {
+          const int ch = (ct * 32 + (HD < 32 ? l32 % HD : l32)) * E;
+          const float v = to_f32(*reinterpret_cast<const T*>(mine + HALF + jj * RB + (((ch >> 4) ^ vsw(jj)) << 4) + (ch & 15)));
+          o[ct] = __builtin_amdgcn_mfma_f32_32x32x2f32(vch ? v : 0.f, s[r], o[ct], 0, 0, 0);
+        }
+      }
     } else {
 #pragma unroll
       for (int kk = 0; kk < 32; ++kk) {
         // key j0 + kk: register (kk / 8) * 4 + kk % 4 of lane half (kk / 4) % 2
         const float p = __shfl(s[(kk >> 3) * 4 + (kk & 3)], l32 + 32 * ((kk >> 2) & 1), 64);
-        if (j0 + kk < lim && there[kk >> 4]) {
-          const T* vp = base[kk >> 4] + (kk & 15) * rs + a.at.kvd;
+        if (j0 + kk < lim) {
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int c = ct * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-              if (c < HD) o[ct][r] = fmaf(p, to_f32(vp[c]), o[ct][r]);
+            for (int r = 0; r < 16; r += 4) {
+              const int c = ct * 32 + 2 * r + 4 * half, ch = c * E;
+              if (c >= HD) continue;
+              const float4 v = load4<T>(reinterpret_cast<const T*>(mine + HALF + kk * RB + (((ch >> 4) ^ vsw(kk)) << 4) + (ch & 15)));
+              o[ct][r] = fmaf(p, v.x, o[ct][r]);
+              o[ct][r + 1] = fmaf(p, v.y, o[ct][r + 1]);
+              o[ct][r + 2] = fmaf(p, v.z, o[ct][r + 2]);
+              o[ct][r + 3] = fmaf(p, v.w, o[ct][r + 3]);
             }
         }
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) load(jn, pg0, pg1, lds0 + HALF, vcol, voff);
   }
   l_run = half_swap_sum(l_run);
+  __syncthreads();  // every wave is past its tiles
+  float* so = reinterpret_cast<float*>(smem);
   if (half == 0) {
     sm[wave][l32] = m_run;
     sl[wave][l32] = l_run;
   }
+  const int nr = min(32, sp.rows - i0);
+  if (l32 < nr) {
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
+    for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int c = ct * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-      if (c < HD) so[wave][c * HP + l32] = o[ct][r];
-    }
+      for (int r = 0; r < 16; ++r) {
+        const int c = ct * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+        if (c < HD) so[(wave * HD + c) * HP + l32] = o[ct][r];
+      }
+  }
   __syncthreads();
-  for (int it = tid; it < 32 * (HD / 4); it += 64 * NW) {
+  for (int it = tid; it < nr * (HD / 4); it += 64 * NW) {
     const int q = it / (HD / 4), c0 = (it % (HD / 4)) * 4, i = i0 + q;
-    if (i >= sp.rows) continue;
     float m = sm[0][q];
 #pragma unroll
     for (int w = 1; w < NW; ++w) m = fmaxf(m, sm[w][q]);
     float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      // a wave without keys for this query holds the empty sum
+      // a wave without keys for this row holds the empty sum
       if (sm[w][q] == -INFINITY && sl[w][q] == 0.f) continue;
       const float f = expf(sm[w][q] - (m == -INFINITY ? 0.f : m));
       l = fmaf(f, sl[w][q], l);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = fmaf(f, so[w][(c0 + e) * HP + q], v[e]);
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(f, so[(w * HD + c0 + e) * HP + q], v[e]);
     }
     const int t = sp.lo + i / a.G, h = g * a.G + i % a.G;
     const int64_t row0 = static_cast<int64_t>(t) * a.H + h;
@@ -1165,12 +1275,31 @@ bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 64; }
 
 // Splits of the keys. The few-row kernels: enough workgroups for four a CU, of
 // 512 keys at least: a second split needs the parts joined, which takes as long
-// (4 sequences of up to 300 rows, 12 heads of 64: 10.9 us, in splits of 128 14.9). The many-row kernel: two a CU, of 512 keys at least (a
-// split's part is as many bytes as 256 of its keys).
-int paged_chunk(bool many, int max_len, int64_t workgroups, int* splits) {
-  const int least = 512;
-  const int64_t blocks = std::max(1, (max_len + least - 1) / least), wgs = std::max<int64_t>(workgroups, 1);
-  const int64_t want = std::min(blocks, std::max<int64_t>(1, ((many ? 2 : 4) * static_cast<int64_t>(device_cu_count()) + wgs - 1) / wgs));
+// (4 sequences of up to 300 rows, 12 heads of 64: 10.9 us, in splits of 128 14.9).
+// The many-row kernel, whose workgroups are long and few a CU: the number whose
+// rounds over the CUs take least, with the parts' bytes. A workgroup takes 8 us
+// and 1.8 us for 64 keys of 128, or, two a CU, 2.9 of 64; parts are written
+// and read at 4 TB/s, and a join that nothing else needs is 4 us.
+int paged_chunk(bool many, int hd, int max_len, int64_t workgroups, bool joined, int* splits) {
+  const int64_t wgs = std::max<int64_t>(workgroups, 1), cus = device_cu_count();
+  const int least = many ? 256 : 512;
+  const int64_t blocks = std::max(1, (max_len + least - 1) / least);
+  int64_t want = std::min(blocks, std::max<int64_t>(1, (4 * cus + wgs - 1) / wgs));
+  if (many) {
+    const double slots = (hd == 64 ? 2.0 : 1.0) * std::max<int64_t>(cus, 1), key = (hd == 64 ? 2.9 : 1.8) / 64;
+    const double part = static_cast<double>(wgs) * kPagedManyRows * hd * 8 / 4e6;
+    double best = 0;
+    for (int64_t n = 1; n <= std::min<int64_t>(blocks, 64); ++n) {
+      const int64_t per = (blocks + n - 1) / n;
+      const bool parts = n > 1 || joined;
+      const double us = ceil(wgs * n / slots) * (std::min<double>(per * least, max_len) * key + 8) + (parts ? n * part : 0) +
+                        (parts && !joined ? 4 : 0);
+      if (n == 1 || us < best) {
+        best = us;
+        want = n;
+      }
+    }
+  }
   const int per = static_cast<int>((blocks + want - 1) / want);
   *splits = static_cast<int>((blocks + per - 1) / per);
   return per * least;
@@ -1181,24 +1310,31 @@ int64_t paged_blocks(const PagedAttention& a, bool many) {
   return (many ? (pairs + 7) / 8 * 8 : pairs) * a.tiles;
 }
 
-hipError_t launch_paged_attention(hipStream_t s, int dtype, bool many, const PagedAttention* job, int jobs) {
-  if (jobs == 0) return hipSuccess;
-  PagedJobs w{};
-  w.job[0] = job[0];
-  w.job[1] = job[jobs - 1];
-  w.first = static_cast<uint32_t>(paged_blocks(job[0], many));
-  const dim3 g(w.first + (jobs > 1 ? static_cast<uint32_t>(paged_blocks(job[1], many)) : 0u));
-  const int hd = job[0].hd;
-  if (many) {
-    if (hd == 64) return launch(K_ATTENTION, paged_many_kernel<64, 2, 4>, g, dim3(256), 0, s, w);
-    return launch(K_ATTENTION, paged_many_kernel<128, 1, 8>, g, dim3(512), 0, s, w);
+hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention* few, int fews,
+                                  const PagedAttention* many, int manys) {
+  PagedJobs w[2] = {};
+  for (int k = 0; k < 2; ++k) {
+    const PagedAttention* job = k ? many : few;
+    const int n = k ? manys : fews;
+    if (n == 0) continue;
+    w[k].job[0] = job[0];
+    w[k].job[1] = job[n - 1];
+    w[k].first = static_cast<uint32_t>(paged_blocks(job[0], k != 0));
+    w[k].blocks = w[k].first + (n > 1 ? static_cast<uint32_t>(paged_blocks(job[1], k != 0)) : 0u);
   }
+  const int hd = (manys > 0 ? many : few)[0].hd;
+  if (manys > 0) {
+    if (hd == 64)
+      return launch(K_ATTENTION, paged_many_kernel<64, 2, 4>, dim3(w[1].blocks + w[0].blocks), dim3(256), 0, s, w[1], w[0]);
+    return launch(K_ATTENTION, paged_many_kernel<128, 1, 8>, dim3(w[1].blocks + (w[0].blocks + 1) / 2), dim3(512), 0, s, w[1], w[0]);
+  }
+  const dim3 g(w[0].blocks);
   if (paged_matrix(dtype, hd)) {
-    if (hd == 64) return launch(K_ATTENTION, paged_few_kernel<64>, g, dim3(256), 0, s, w);
-    return launch(K_ATTENTION, paged_few_kernel<128>, g, dim3(256), 0, s, w);
+    if (hd == 64) return launch(K_ATTENTION, paged_few_kernel<64>, g, dim3(256), 0, s, w[0]);
+    return launch(K_ATTENTION, paged_few_kernel<128>, g, dim3(256), 0, s, w[0]);
   }
-  if (dtype == 1) return f32_dispatch<bf16_t>(s, w, g);
-  return f32_dispatch<float>(s, w, g);
+  if (dtype == 1) return f32_dispatch<bf16_t>(s, w[0], g);
+  return f32_dispatch<float>(s, w[0], g);
 }
 
 hipError_t launch_paged_join(hipStream_t s, int dtype, const float2* ml, const float* o, int parts, int T, int H,

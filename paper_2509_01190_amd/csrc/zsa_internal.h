@@ -473,11 +473,12 @@ struct PagedAttention {
 };
 constexpr int kPagedManyRows = 256, kPagedFewRows = 32;  // packed rows of a workgroup
 bool paged_matrix(int dtype, int hd);  // the bf16 matrix kernels take these heads: one for few rows, one for many
-// keys a split of up to max_len rows takes, and how many splits that makes
-int paged_chunk(bool many, int max_len, int64_t workgroups, int* splits);
+// keys a split of up to max_len rows takes, and how many splits that makes; joined: rows have other parts anyway
+int paged_chunk(bool many, int hd, int max_len, int64_t workgroups, bool joined, int* splits);
 int64_t paged_blocks(const PagedAttention& a, bool many);  // workgroups
-// one launch of up to two of them, of one type and kind
-hipError_t launch_paged_attention(hipStream_t s, int dtype, bool many, const PagedAttention* job, int jobs);
+// one launch of up to two of each kind, of one type and head dim
+hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention* few, int fews,
+                                  const PagedAttention* many, int manys);
 hipError_t launch_paged_join(hipStream_t s, int dtype, const float2* ml, const float* o, int parts, int T, int H,
                              int hd, void* out, int64_t out_stride, float* lse);
 

@@ -105,11 +105,11 @@ struct Plan {
 
 int tile_of(bool many) { return many ? zsa::kPagedManyRows : zsa::kPagedFewRows; }
 
-Part part_of(bool many, int64_t max_rows, int64_t workgroups, int max_len) {
+Part part_of(bool many, int hd, int64_t max_rows, int64_t workgroups, int max_len, bool joined) {
   Part l{};
   l.many = many;
   l.tiles = static_cast<int>((max_rows + tile_of(many) - 1) / tile_of(many));
-  l.chunk = zsa::paged_chunk(many, max_len, workgroups, &l.splits);
+  l.chunk = zsa::paged_chunk(many, hd, max_len, workgroups, joined, &l.splits);
   return l;
 }
 
@@ -124,11 +124,11 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
     most[many] = std::max(most[many], rows);
     tiles[many] += (rows + tile_of(many) - 1) / tile_of(many);
   }
-  if (most[0] > 0) p.few = part_of(false, most[0], tiles[0] * kv.n_kv_heads, max_len);
-  if (most[1] > 0) p.many = part_of(true, most[1], tiles[1] * kv.n_kv_heads, max_len);
+  if (most[0] > 0) p.few = part_of(false, kv.head_dim, most[0], tiles[0] * kv.n_kv_heads, max_len, prefix > 0);
+  if (most[1] > 0) p.many = part_of(true, kv.head_dim, most[1], tiles[1] * kv.n_kv_heads, max_len, prefix > 0);
   if (prefix > 0) {
     const bool many = matrix && T * G > kFewRows;
-    p.prefix = part_of(many, T * G, (T * G + tile_of(many) - 1) / tile_of(many) * kv.n_kv_heads, prefix);
+    p.prefix = part_of(many, kv.head_dim, T * G, (T * G + tile_of(many) - 1) / tile_of(many) * kv.n_kv_heads, prefix, true);
   }
   return p;
 }
@@ -186,7 +186,7 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
   a.out = out;
   a.out_stride = out_stride;
   a.lse = lse;
-  // the launches: of the few-row kernel and of the many-row one
+  // the work of the few-row kernel and of the many-row one
   zsa::PagedAttention job[2][2];
   int jobs[2] = {0, 0};
   for (const Part* l : {&p.prefix, &p.few, &p.many}) {
@@ -218,8 +218,7 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
       return set_error(ZSA_EUNSUPPORTED, "%d sequences of up to %d rows of %d heads: more workgroups than a grid holds",
                        batch, max_new, n_heads);
   }
-  for (int many = 1; many >= 0; --many)
-    HIP_TRY(zsa::launch_paged_attention(s, kv->dtype, many != 0, job[many], jobs[many]), "paged attention");
+  HIP_TRY(zsa::launch_paged_attention(s, kv->dtype, job[0], jobs[0], job[1], jobs[1]), "paged attention");
   if (p.join())
     HIP_TRY(zsa::launch_paged_join(s, kv->dtype, ml, o, p.parts(), T, n_heads, kv->head_dim, out, out_stride, lse),
             "paged attention's parts");
