@@ -26,6 +26,7 @@ namespace zsa {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -140,6 +141,17 @@ __device__ __forceinline__ Span span_of(const PagedAttention& a, int b) {
   return s;
 }
 
+// the maximum and the sum over the lanes l % 16 (half_swap_max goes on from
+// rows of 16 lanes swapped in pairs)
+__device__ __forceinline__ float quarter_swap_max(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return half_swap_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quarter_swap_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return half_swap_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
 // A launch's work: the common prefix's and the sequences' own, if both are of
 // one kind. The prefix's workgroups, which have more to do, come first.
 struct PagedJobs {
@@ -168,29 +180,30 @@ __device__ __forceinline__ scalar_ids scalar(const int32_t* p) {
 // XCD L % 8: with the splits fastest and 2, 4 or 8 of them a ragged batch's
 // last splits, mostly empty, were all on the same XCDs.
 
-// bf16, heads of 64 and 128, up to 32 packed rows at a time: bound by the
-// cached rows' bytes. A workgroup takes 32 packed rows of one (sequence,
+// bf16, heads of 64 and 128, 16 packed rows at a time: bound by the
+// cached rows' bytes. A workgroup takes 16 packed rows of one (sequence,
 // key/value head) and a split of its keys; its four waves take 32-key tiles in
 // turn, each through its own K and V buffer in LDS, without barriers: the next
 // tile's K is under way as soon as S^T = K Q^T has read the last one, its V
 // after O^T += V^T P^T has. A load instruction covers whole rows of a head (4
 // of 128, 8 of 64) of one page, through a buffer resource that ends with the
 // sequence, so what lies behind its last row reads as zeros, and so does a
-// page outside the pool. The transposed products leave a lane the scores of
-// one row, which are the operand of the second product (k_attn.hip). P meets V
-// as two bf16 numbers whose sum has 16 bits: the matrix cores have the time.
+// page outside the pool. The transposed products leave a lane eight scores of
+// one row, keys 4 (l / 16) + r and those + 16, which are its operand of the
+// second product; V is read in that same order of keys. P meets V as two bf16
+// numbers whose sum has 16 bits: the matrix cores have the time.
 template <int HD>
 struct FewShared {  // LDS of a group of four waves
-  static constexpr int NW = 4, HP = 33;  // merge row stride: [channel][row]
+  static constexpr int NW = 4, HP = 17;  // merge row stride: [channel][row]
   static constexpr int TILES = NW * 64 * HD * 2, MERGE = NW * HD * HP * 4;
   unsigned char tiles[MERGE > TILES ? MERGE : TILES];
-  float m[NW][32], l[NW][32];
+  float m[NW][16], l[NW][16];
 };
 
 // the work of one of `blocks` groups of four waves, as its thread `tid`; all threads of the workgroup call it
 template <int HD>
 __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, bool there, int tid, FewShared<HD>& shared) {
-  constexpr int NW = FewShared<HD>::NW, KK = HD / 16, CT = HD / 32, CPR = HD / 8;
+  constexpr int NW = FewShared<HD>::NW, KK = HD / 32, CT = HD / 16, CPR = HD / 8;
   constexpr int RB = HD * 2, HALF = 32 * RB;    // a tile of 32 rows of K, or V
   constexpr int RPL = 1024 / RB, NL = 16 / RPL;  // rows a load, loads per 16 rows
   constexpr int HP = FewShared<HD>::HP;
@@ -200,14 +213,14 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
   const int Hkv = a.H / a.G, pair = block % (Hkv * a.B), st = block / (Hkv * a.B);
   const int g = pair % Hkv, b = pair / Hkv, tile = st % a.tiles, split = st / a.tiles;
   const Span sp = span_of(a, b);
-  const int i0 = tile * 32;
+  const int i0 = tile * kPagedFewRows;
   const bool live = there && i0 < sp.rows && sp.rows <= a.few_rows;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int half = lane >> 5, l32 = lane & 31;
-  const int row = min(i0 + l32, sp.rows - 1);  // rows past the sequence are not stored
+  const int quarter = lane >> 4, l16 = lane & 15;
+  const int row = min(i0 + l16, sp.rows - 1);  // rows past the sequence are not stored
   const int lim = a.causal ? min(sp.first + row / a.G, sp.len) : sp.len;
   const int lim0 = a.causal ? min(sp.first + i0 / a.G, sp.len) : sp.len;  // the tile's first row's
-  const int last = a.causal ? min(sp.first + min(i0 + 31, sp.rows - 1) / a.G, sp.len) : sp.len;
+  const int last = a.causal ? min(sp.first + min(i0 + 15, sp.rows - 1) / a.G, sp.len) : sp.len;
   const int k0 = split * a.chunk, kend = live ? min(last, k0 + a.chunk) : 0;
   const float scale_log2 = a.scale * kLog2e;
 
@@ -249,16 +262,14 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
   };
 
   float m_run = -INFINITY, l_run = 0.f;  // of the raw scores; l_run: this lane's keys only
-  f32x16_t o[CT];
+  const f32x4_t zero = {};
+  f32x4_t o[CT];
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
-  // fragment addresses (k_attn.hip)
-  const uint32_t vrow = 4 * half + ((lane & 15) >> 2);
-  const int ks0 = ksw(l32), vs0 = vsw(vrow);
-  const int vch = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-  const f32x16_t zero = {};
+  for (int ct = 0; ct < CT; ++ct) o[ct] = zero;
+  // fragment addresses: a transposing read gives group `quarter` of 16 lanes
+  // the keys 4 quarter .. + 3 of 16 channels, one a lane
+  const uint32_t vrow = 4 * quarter + (l16 >> 2);
+  const int ks0 = ksw(l16), vs0 = vsw(vrow);
 
   int j0 = k0 + wave * 32;
   int pg0 = page_of(j0), pg1 = page_of(j0 + 16);
@@ -272,7 +283,7 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
                        (g * a.G + row % a.G) * HD;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
-      qf[kk] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(qp + kk * 16 + half * 8));
+      qf[kk] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(qp + kk * 32 + quarter * 8));
     // here before the loop, which would otherwise wait for every load in it
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]));
@@ -284,26 +295,28 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
     pg1 = page_of(jn + 16);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // K is here, V may be under way
     __builtin_amdgcn_sched_barrier(0);
-    f32x16_t s;
+    f32x4_t s[2];
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      const bf16x8_t k = __builtin_bit_cast(
-          bf16x8_t, *reinterpret_cast<const u32x4*>(mine + l32 * RB + (((2 * kk + half) ^ ks0) << 4)));
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[kk], kk == 0 ? zero : s, 0, 0, 0);
-    }
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16x8_t k = __builtin_bit_cast(
+            bf16x8_t, *reinterpret_cast<const u32x4*>(mine + (16 * t + l16) * RB + (((4 * kk + quarter) ^ ks0) << 4)));
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[kk], kk == 0 ? zero : s[t], 0, 0, 0);
+      }
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) load(jn, pg0, pg1, lds0, kcol, koff);
-    // s[r]: key j0 + 8 (r/4) + 4 half + r%4, packed row `row`
+    // s[t][r]: key j0 + 16 t + 4 quarter + r, packed row `row`
     if (j0 + 32 > lim0) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (j0 + 8 * (r >> 2) + 4 * half + (r & 3) >= lim) s[r] = -INFINITY;
-    }
-    float mloc = s[0];
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mloc = fmaxf(mloc, s[r]);
-    mloc = half_swap_max(mloc);
+        for (int r = 0; r < 4; ++r)
+          if (j0 + 16 * t + 4 * quarter + r >= lim) s[t][r] = -INFINITY;
+    }
+    const float mloc = quarter_swap_max(fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                                              fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))));
     // the reference maximum moves only when it has to (k_attn.hip)
     const float m_new = fmaxf(m_run, mloc);
     if (__builtin_amdgcn_ballot_w64(m_new == -INFINITY ? false : !((m_new - m_run) * scale_log2 <= 8.0f)) != 0) {
@@ -312,22 +325,24 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
+        for (int r = 0; r < 4; ++r) o[ct][r] *= alpha;
       m_run = m_new;
     }
     const float m_use = m_run == -INFINITY ? 0.f : m_run * scale_log2;
-    u32x4 hi[2], lo[2];
+    u32x4 hi, lo;
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[r], scale_log2, -m_use));
-      const float p1 = __builtin_amdgcn_exp2f(fmaf(s[r + 1], scale_log2, -m_use));
-      l_run += p0 + p1;
-      s[r] = p0;
-      s[r + 1] = p1;
-      const uint32_t w = pack_bf16x2(p0, p1);
-      hi[r >> 3][(r >> 1) & 3] = w;
-      lo[r >> 3][(r >> 1) & 3] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u));
-    }
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t][r], scale_log2, -m_use));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[t][r + 1], scale_log2, -m_use));
+        l_run += p0 + p1;
+        s[t][r] = p0;
+        s[t][r + 1] = p1;
+        const uint32_t w = pack_bf16x2(p0, p1);
+        hi[2 * t + (r >> 1)] = w;
+        lo[2 * t + (r >> 1)] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u));
+      }
     if (more)
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // V is here, the next K may be under way
     else
@@ -349,31 +364,27 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
     }
     if (!odd) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          const unsigned char* vr = mine + HALF + (16 * k + vrow) * RB + (lane & 1) * 8 + (((4 * ct + vch) ^ vs0) << 4);
-          const bf16x8_t v = __builtin_bit_cast(bf16x8_t, lds_read_columns(vr, vr + 8 * RB));
-          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, hi[k]), o[ct], 0, 0, 0);
-          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, lo[k]), o[ct], 0, 0, 0);
-        }
+      for (int ct = 0; ct < CT; ++ct) {
+        const unsigned char* vr = mine + HALF + vrow * RB + (lane & 1) * 8 + (((2 * ct + ((lane >> 1) & 1)) ^ vs0) << 4);
+        const bf16x8_t v = __builtin_bit_cast(bf16x8_t, lds_read_columns(vr, vr + 16 * RB));
+        o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, hi), o[ct], 0, 0, 0);
+        o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, lo), o[ct], 0, 0, 0);
+      }
     } else {
 #pragma unroll
       for (int kk = 0; kk < 32; ++kk) {
-        // key j0 + kk: register (kk / 8) * 4 + kk % 4 of lane half (kk / 4) % 2
-        const float p = __shfl(s[(kk >> 3) * 4 + (kk & 3)], l32 + 32 * ((kk >> 2) & 1), 64);
+        // key j0 + kk: register kk % 4 of tile kk / 16, lane quarter (kk / 4) % 4
+        const float p = __shfl(s[kk >> 4][kk & 3], l16 + 16 * ((kk >> 2) & 3), 64);
         if (j0 + kk < lim) {
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-              const int c = ct * 32 + 2 * r + 4 * half;
-              const uint2 w = *reinterpret_cast<const uint2*>(mine + HALF + kk * RB + (((c >> 3) ^ vsw(kk)) << 4) + (c & 7) * 2);
-              o[ct][r] = fmaf(p, __uint_as_float(w.x << 16), o[ct][r]);
-              o[ct][r + 1] = fmaf(p, __uint_as_float(w.x & 0xffff0000u), o[ct][r + 1]);
-              o[ct][r + 2] = fmaf(p, __uint_as_float(w.y << 16), o[ct][r + 2]);
-              o[ct][r + 3] = fmaf(p, __uint_as_float(w.y & 0xffff0000u), o[ct][r + 3]);
-            }
+          for (int ct = 0; ct < CT; ++ct) {
+            const int c = ct * 16 + 4 * quarter;
+            const uint2 w = *reinterpret_cast<const uint2*>(mine + HALF + kk * RB + (((c >> 3) ^ vsw(kk)) << 4) + (c & 7) * 2);
+            o[ct][0] = fmaf(p, __uint_as_float(w.x << 16), o[ct][0]);
+            o[ct][1] = fmaf(p, __uint_as_float(w.x & 0xffff0000u), o[ct][1]);
+            o[ct][2] = fmaf(p, __uint_as_float(w.y << 16), o[ct][2]);
+            o[ct][3] = fmaf(p, __uint_as_float(w.y & 0xffff0000u), o[ct][3]);
+          }
         }
       }
     }
@@ -381,20 +392,19 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) load(jn, pg0, pg1, lds0 + HALF, vcol, voff);
   }
-  l_run = half_swap_sum(l_run);
+  l_run = quarter_swap_sum(l_run);
   __syncthreads();  // every wave is past its tiles
   float* so = reinterpret_cast<float*>(smem);
-  if (half == 0) {
-    sm[wave][l32] = m_run == -INFINITY ? -INFINITY : m_run * scale_log2;
-    sl[wave][l32] = l_run;
+  if (quarter == 0) {
+    sm[wave][l16] = m_run == -INFINITY ? -INFINITY : m_run * scale_log2;
+    sl[wave][l16] = l_run;
   }
-  const int nr = live ? min(32, sp.rows - i0) : 0;
-  if (l32 < nr) {
+  const int nr = live ? min(kPagedFewRows, sp.rows - i0) : 0;
+  if (l16 < nr) {
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        so[(wave * HD + ct * 32 + 8 * (r >> 2) + 4 * half + (r & 3)) * HP + l32] = o[ct][r];
+      for (int r = 0; r < 4; ++r) so[(wave * HD + ct * 16 + 4 * quarter + r) * HP + l16] = o[ct][r];
   }
   __syncthreads();
   for (int it = tid; it < nr * (HD / 4); it += 64 * NW) {
@@ -898,27 +908,30 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 }
 
 // fp32 storage, and bf16 at head dims 16 and 32: the few-row kernel with both
-// products on v_mfma_f32_32x32x2_f32, fp32 operands and sums, for any number of
-// packed rows, 32 at a time. K is read from LDS 16 bytes a lane, as the first
-// operand has it; V one number a lane, 32 consecutive channels a half-wave. The
+// products on the fp32 matrix instructions, fp32 operands and sums, for any
+// number of packed rows, W = 16 or 32 at a time (one row costs what W do). K is read from LDS 16 bytes a lane, as the first
+// operand has it; V one number a lane, W consecutive channels a row. The
 // exponentials are expf (the fp32 attention in k_attn.hip says why).
-template <typename T, int HD>
+template <typename T, int HD, int W>
 struct F32Shared {
-  static constexpr int NW = 4, HP = 33;  // merge row stride: [channel][row]
+  static constexpr int NW = 4, HP = W + 1;  // merge row stride: [channel][row]
   static constexpr int TILES = NW * 64 * HD * sizeof(T), MERGE = NW * HD * HP * 4;
   unsigned char tiles[MERGE > TILES ? MERGE : TILES];
-  float m[NW][32], l[NW][32];
+  float m[NW][W], l[NW][W];
 };
 
-template <typename T, int HD>
+template <typename T, int HD, int W>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 1 : HD == 64 ? 2 : 3))) void paged_f32_kernel(
     PagedJobs jobs) {
-  constexpr int NW = 4, E = sizeof(T), KK = HD / 8;
-  constexpr int CT = HD < 32 ? 1 : HD / 32;  // 32-channel blocks of O (half empty at HD 16)
+  constexpr int NW = 4, E = sizeof(T);
+  constexpr int NG = 64 / W, NT = 32 / W, NR = W * W / 64;  // lane groups, key tiles of a step, registers of a tile
+  constexpr int KK = HD / (4 * NG);          // channels go 4 a lane and group
+  constexpr int CT = HD < W ? 1 : HD / W;    // W-channel blocks of O (half empty at HD 16, W 32)
+  typedef std::conditional_t<W == 32, f32x16_t, f32x4_t> acc_t;
   constexpr int RB = HD * E, HALF = 32 * RB, CPR = RB / 16;
   constexpr int RPL = 1024 / RB < 16 ? 1024 / RB : 16, NL = 16 / RPL;  // rows a load, loads per 16 rows
-  constexpr int HP = F32Shared<T, HD>::HP;
-  __shared__ __align__(1024) F32Shared<T, HD> shared;
+  constexpr int HP = F32Shared<T, HD, W>::HP;
+  __shared__ __align__(1024) F32Shared<T, HD, W> shared;
   unsigned char* smem = shared.tiles;
   auto& sm = shared.m;
   auto& sl = shared.l;
@@ -927,21 +940,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
   const int Hkv = a.H / a.G, pair = block % (Hkv * a.B), st = block / (Hkv * a.B);
   const int g = pair % Hkv, b = pair / Hkv, tile = st % a.tiles, split = st / a.tiles;
   const Span sp = span_of(a, b);
-  const int i0 = tile * 32;
+  const int i0 = tile * W;
   if (i0 >= sp.rows) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int half = lane >> 5, l32 = lane & 31;
-  const int row = min(i0 + l32, sp.rows - 1);  // rows past the sequence are not stored
+  const int group = lane / W, col = lane % W;
+  const int row = min(i0 + col, sp.rows - 1);  // rows past the sequence are not stored
   const int lim = a.causal ? min(sp.first + row / a.G, sp.len) : sp.len;
   const int lim0 = a.causal ? min(sp.first + i0 / a.G, sp.len) : sp.len;  // the tile's first row's
-  const int last = a.causal ? min(sp.first + min(i0 + 31, sp.rows - 1) / a.G, sp.len) : sp.len;
+  const int last = a.causal ? min(sp.first + min(i0 + W - 1, sp.rows - 1) / a.G, sp.len) : sp.len;
   const int k0 = split * a.chunk, kend = min(last, k0 + a.chunk);
 
   // K row r of a tile keeps its 16-byte chunk c at c ^ ksw(r): the rows of a
   // read phase fall on all banks; V row r at c ^ vsw(r): rows four apart, which
-  // the two half-waves read at once, do
+  // the lane groups read at once, do
   auto ksw = [](int r) { return CPR >= 16 ? r & 15 : CPR == 8 ? (r >> 1) & 7 : CPR == 4 ? (r >> 2) & 3 : (r >> 3) & 1; };
-  auto vsw = [](int r) { return CPR >= 16 ? ((r >> 2) & 1) << 3 : 0; };
+  auto vsw = [](int r) { return CPR >= 16 ? ((r >> 2) & (NG - 1)) << (W == 32 ? 3 : 2) : CPR == 8 && W == 16 ? ((r >> 2) & 1) << 2 : 0; };
   const uint32_t rowb = static_cast<uint32_t>(a.at.kvd) * (2 * E);
   uint32_t koff[NL], voff[NL];
 #pragma unroll
@@ -978,13 +991,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
   };
 
   float m_run = -INFINITY, l_run = 0.f;  // of the scaled scores; l_run: this lane's keys only
-  f32x16_t o[CT];
+  const acc_t zero = {};
+  acc_t o[CT];
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
-  const bool vch = HD >= 32 || l32 < HD;  // lanes whose channel exists
-  const int ks0 = ksw(l32);
+  for (int ct = 0; ct < CT; ++ct) o[ct] = zero;
+  const bool vch = HD >= W || col < HD;  // lanes whose channel exists
+  // the key of register r of tile t; the same of the channel of a register of O
+  auto key = [&](int t, int r) { return t * W + 8 * (r >> 2) + 4 * group + (r & 3); };
+  auto mfma = [](float x, float y, acc_t c) {
+    if constexpr (W == 32) return __builtin_amdgcn_mfma_f32_32x32x2f32(x, y, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x4f32(x, y, c, 0, 0, 0);
+  };
   int j0 = k0 + wave * 32;
   int pg0 = page_of(j0), pg1 = page_of(j0 + 16);
   if (j0 < kend) {
@@ -995,7 +1012,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
   if (j0 < kend) {
     const T* qp = static_cast<const T*>(a.q) + static_cast<int64_t>(sp.lo + row / a.G) * a.q_stride + (g * a.G + row % a.G) * HD;
 #pragma unroll
-    for (int s = 0; s < KK; ++s) qf[s] = load4<T>(qp + 8 * s + 4 * half);
+    for (int s = 0; s < KK; ++s) qf[s] = load4<T>(qp + 4 * (NG * s + group));
     // here before the loop, which would otherwise wait for every load in it
 #pragma unroll
     for (int s = 0; s < KK; ++s) asm volatile("" : "+v"(qf[s].x), "+v"(qf[s].y), "+v"(qf[s].z), "+v"(qf[s].w));
@@ -1007,29 +1024,31 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
     pg1 = page_of(jn + 16);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // K is here, V may be under way
     __builtin_amdgcn_sched_barrier(0);
-    f32x16_t s = {};
+    acc_t s[NT];
 #pragma unroll
-    for (int t = 0; t < KK; ++t) {
-      const int ch = (8 * t + 4 * half) * E;  // byte of the lane's four channels in a row
-      const float4 k4 = load4<T>(reinterpret_cast<const T*>(mine + l32 * RB + (((ch >> 4) ^ ks0) << 4) + (ch & 15)));
-      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, qf[t].x, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, qf[t].y, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.z, qf[t].z, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.w, qf[t].w, s, 0, 0, 0);
-    }
+    for (int c = 0; c < KK; ++c)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int kr = t * W + col, ch = 4 * (NG * c + group) * E;  // byte of the lane's four channels in a row
+        const float4 k4 = load4<T>(reinterpret_cast<const T*>(mine + kr * RB + (((ch >> 4) ^ ksw(kr)) << 4) + (ch & 15)));
+        s[t] = mfma(k4.x, qf[c].x, c == 0 ? zero : s[t]);
+        s[t] = mfma(k4.y, qf[c].y, s[t]);
+        s[t] = mfma(k4.z, qf[c].z, s[t]);
+        s[t] = mfma(k4.w, qf[c].w, s[t]);
+      }
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) load(jn, pg0, pg1, lds0, kcol, koff);
-    // s[r]: key j0 + 8 (r/4) + 4 half + r%4, packed row `row`
     const bool edge = j0 + 32 > lim0;
     float mloc = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int j = j0 + 8 * (r >> 2) + 4 * half + (r & 3);
-      s[r] = edge && j >= lim ? -INFINITY : s[r] * a.scale;
-      mloc = fmaxf(mloc, s[r]);
-    }
-    mloc = half_swap_max(mloc);
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        s[t][r] = edge && j0 + key(t, r) >= lim ? -INFINITY : s[t][r] * a.scale;
+        mloc = fmaxf(mloc, s[t][r]);
+      }
+    mloc = W == 32 ? half_swap_max(mloc) : quarter_swap_max(mloc);
     const float m_new = fmaxf(m_run, mloc);
     if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {
       const float alpha = m_new == -INFINITY ? 1.0f : expf(m_run - m_new);
@@ -1037,15 +1056,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
+        for (int r = 0; r < NR; ++r) o[ct][r] *= alpha;
       m_run = m_new;
     }
     const float m_use = m_run == -INFINITY ? 0.f : m_run;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = expf(s[r] - m_use);
-      l_run += s[r];
-    }
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        s[t][r] = expf(s[t][r] - m_use);
+        l_run += s[t][r];
+      }
     if (more)
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // V is here, the next K may be under way
     else
@@ -1065,26 +1086,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
     }
     if (!odd) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int jj = 8 * (r >> 2) + 4 * half + (r & 3);
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          const int ch = (ct * 32 + (HD < 32 ? l32 % HD : l32)) * E;
-          const float v = to_f32(*reinterpret_cast<const T*>(mine + HALF + jj * RB + (((ch >> 4) ^ vsw(jj)) << 4) + (ch & 15)));
-          o[ct] = __builtin_amdgcn_mfma_f32_32x32x2f32(vch ? v : 0.f, s[r], o[ct], 0, 0, 0);
+        for (int r = 0; r < NR; ++r) {
+          const int jj = key(t, r);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            const int ch = (ct * W + (HD < W ? col % HD : col)) * E;
+            const float v = to_f32(*reinterpret_cast<const T*>(mine + HALF + jj * RB + (((ch >> 4) ^ vsw(jj)) << 4) + (ch & 15)));
+            o[ct] = mfma(vch ? v : 0.f, s[t][r], o[ct]);
+          }
         }
-      }
     } else {
 #pragma unroll
       for (int kk = 0; kk < 32; ++kk) {
-        // key j0 + kk: register (kk / 8) * 4 + kk % 4 of lane half (kk / 4) % 2
-        const float p = __shfl(s[(kk >> 3) * 4 + (kk & 3)], l32 + 32 * ((kk >> 2) & 1), 64);
+        const int w = kk % W;  // key j0 + kk: its register, and its lane group
+        const float p = __shfl(s[kk / W][W == 32 ? (w >> 3) * 4 + (w & 3) : w & 3], col + W * ((w >> 2) & (NG - 1)), 64);
         if (j0 + kk < lim) {
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-              const int c = ct * 32 + 2 * r + 4 * half, ch = c * E;
+            for (int r = 0; r < NR; r += 4) {
+              const int c = ct * W + 2 * r + 4 * group, ch = c * E;
               if (c >= HD) continue;
               const float4 v = load4<T>(reinterpret_cast<const T*>(mine + HALF + kk * RB + (((ch >> 4) ^ vsw(kk)) << 4) + (ch & 15)));
               o[ct][r] = fmaf(p, v.x, o[ct][r]);
@@ -1099,22 +1122,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) load(jn, pg0, pg1, lds0 + HALF, vcol, voff);
   }
-  l_run = half_swap_sum(l_run);
+  l_run = W == 32 ? half_swap_sum(l_run) : quarter_swap_sum(l_run);
   __syncthreads();  // every wave is past its tiles
   float* so = reinterpret_cast<float*>(smem);
-  if (half == 0) {
-    sm[wave][l32] = m_run;
-    sl[wave][l32] = l_run;
+  if (group == 0) {
+    sm[wave][col] = m_run;
+    sl[wave][col] = l_run;
   }
-  const int nr = min(32, sp.rows - i0);
-  if (l32 < nr) {
+  const int nr = min(W, sp.rows - i0);
+  if (col < nr) {
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int c = ct * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-        if (c < HD) so[(wave * HD + c) * HP + l32] = o[ct][r];
-      }
+      for (int r = 0; r < NR; ++r)
+        if (key(ct, r) < HD) so[(wave * HD + key(ct, r)) * HP + col] = o[ct][r];
   }
   __syncthreads();
   for (int it = tid; it < nr * (HD / 4); it += 64 * NW) {
@@ -1226,17 +1247,17 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restric
     lse[static_cast<int64_t>(h) * Trows + t] = L == 0.f ? -INFINITY : LOG2 ? (M + log2f(L)) * kLn2 : M + logf(L);
 }
 
-template <typename T>
+template <typename T, int W>
 hipError_t f32_dispatch(hipStream_t s, const PagedJobs& jobs, dim3 g) {
   const dim3 block(256);
   switch (jobs.job[0].hd) {
-    case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16>, g, block, 0, s, jobs);
-    case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32>, g, block, 0, s, jobs);
+    case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16, W>, g, block, 0, s, jobs);
+    case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32, W>, g, block, 0, s, jobs);
     default: break;
   }
   if constexpr (sizeof(T) == 4) {
-    if (jobs.job[0].hd == 64) return launch(K_ATTENTION, paged_f32_kernel<T, 64>, g, block, 0, s, jobs);
-    if (jobs.job[0].hd == 128) return launch(K_ATTENTION, paged_f32_kernel<T, 128>, g, block, 0, s, jobs);
+    if (jobs.job[0].hd == 64) return launch(K_ATTENTION, paged_f32_kernel<T, 64, W>, g, block, 0, s, jobs);
+    if (jobs.job[0].hd == 128) return launch(K_ATTENTION, paged_f32_kernel<T, 128, W>, g, block, 0, s, jobs);
   }
   return hipErrorInvalidValue;
 }
@@ -1333,8 +1354,8 @@ hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention
     if (hd == 64) return launch(K_ATTENTION, paged_few_kernel<64>, g, dim3(256), 0, s, w[0]);
     return launch(K_ATTENTION, paged_few_kernel<128>, g, dim3(256), 0, s, w[0]);
   }
-  if (dtype == 1) return f32_dispatch<bf16_t>(s, w[0], g);
-  return f32_dispatch<float>(s, w[0], g);
+  if (few[0].tile == 32) return dtype == 1 ? f32_dispatch<bf16_t, 32>(s, w[0], g) : f32_dispatch<float, 32>(s, w[0], g);
+  return dtype == 1 ? f32_dispatch<bf16_t, 16>(s, w[0], g) : f32_dispatch<float, 16>(s, w[0], g);
 }
 
 hipError_t launch_paged_join(hipStream_t s, int dtype, const float2* ml, const float* o, int parts, int T, int H,

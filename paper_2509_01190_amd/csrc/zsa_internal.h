@@ -460,7 +460,7 @@ struct PagedAttention {
   int T, B, H, G, hd;
   int causal;
   float scale;
-  int tiles;                  // blocks of packed rows of the longest sequence (kPagedManyRows each, or kPagedFewRows)
+  int tile, tiles;            // packed rows of a workgroup; of the longest sequence, how many of those
   int few_rows;               // a few-row launch takes the sequences of up to so many packed rows, a many-row one the others
   int chunk, splits;          // keys a split takes, a multiple of 128; splits
   int parts;                  // the call's parts from this launch's first on
@@ -471,7 +471,7 @@ struct PagedAttention {
   float2* ml;                 // [part][T * H] maximum and sum of the scores, or null: no row has parts
   float* o;                   // [part][T * H][hd] sums of values
 };
-constexpr int kPagedManyRows = 256, kPagedFewRows = 32;  // packed rows of a workgroup
+constexpr int kPagedManyRows = 256, kPagedFewRows = 16;  // packed rows of a workgroup (the fp32 kernel: 16 or 32)
 bool paged_matrix(int dtype, int hd);  // the bf16 matrix kernels take these heads: one for few rows, one for many
 // keys a split of up to max_len rows takes, and how many splits that makes; joined: rows have other parts anyway
 int paged_chunk(bool many, int hd, int max_len, int64_t workgroups, bool joined, int* splits);

@@ -89,7 +89,7 @@ constexpr int kFewRows = 32;
 // of few packed rows, or of many.
 struct Part {
   bool many;
-  int tiles;          // of the longest sequence
+  int tile, tiles;    // packed rows of a workgroup; of the longest sequence, how many of those
   int chunk, splits;  // 0 splits: there are none
 };
 
@@ -103,32 +103,36 @@ struct Plan {
   bool join() const { return parts() > 1; }
 };
 
-int tile_of(bool many) { return many ? zsa::kPagedManyRows : zsa::kPagedFewRows; }
-
-Part part_of(bool many, int hd, int64_t max_rows, int64_t workgroups, int max_len, bool joined) {
-  Part l{};
-  l.many = many;
-  l.tiles = static_cast<int>((max_rows + tile_of(many) - 1) / tile_of(many));
-  l.chunk = zsa::paged_chunk(many, hd, max_len, workgroups, joined, &l.splits);
-  return l;
-}
-
 Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int max_len, int prefix) {
   Plan p{};
+  const int hd = kv.head_dim;
   const int64_t G = H / kv.n_kv_heads, T = cu[batch];
-  const bool matrix = zsa::paged_matrix(kv.dtype, kv.head_dim);
-  int64_t most[2] = {0, 0}, tiles[2] = {0, 0};
+  const bool matrix = zsa::paged_matrix(kv.dtype, hd);
+  int64_t most[2] = {0, 0};
   for (int b = 0; b < batch; ++b) {
     const int64_t rows = (cu[b + 1] - cu[b]) * G;
     const bool many = matrix && rows > kFewRows;
     most[many] = std::max(most[many], rows);
-    tiles[many] += (rows + tile_of(many) - 1) / tile_of(many);
   }
-  if (most[0] > 0) p.few = part_of(false, kv.head_dim, most[0], tiles[0] * kv.n_kv_heads, max_len, prefix > 0);
-  if (most[1] > 0) p.many = part_of(true, kv.head_dim, most[1], tiles[1] * kv.n_kv_heads, max_len, prefix > 0);
+  auto part = [&](bool many, int64_t max_rows, int max_len, bool common) {
+    Part l{};
+    l.many = many;
+    l.tile = many ? zsa::kPagedManyRows : !matrix && max_rows > 16 ? 32 : zsa::kPagedFewRows;
+    l.tiles = static_cast<int>((max_rows + l.tile - 1) / l.tile);
+    int64_t workgroups = common ? l.tiles : 0;
+    for (int b = 0; b < batch && !common; ++b) {
+      const int64_t rows = (cu[b + 1] - cu[b]) * G;
+      if (many == (matrix && rows > kFewRows)) workgroups += (rows + l.tile - 1) / l.tile;
+    }
+    l.chunk = zsa::paged_chunk(many, hd, max_len, workgroups * kv.n_kv_heads, prefix > 0, &l.splits);
+    return l;
+  };
+  if (most[0] > 0) p.few = part(false, most[0], max_len, false);
+  if (most[1] > 0) p.many = part(true, most[1], max_len, false);
   if (prefix > 0) {
-    const bool many = matrix && T * G > kFewRows;
-    p.prefix = part_of(many, kv.head_dim, T * G, (T * G + tile_of(many) - 1) / tile_of(many) * kv.n_kv_heads, prefix, true);
+    // (one launch takes one width of tiles)
+    p.prefix = part(matrix && T * G > kFewRows, T * G, prefix, true);
+    if (!matrix && p.few.splits > 0 && p.few.tile != p.prefix.tile) p.few = part(false, std::max<int64_t>(most[0], 17), max_len, false);
   }
   return p;
 }
@@ -194,6 +198,7 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
     zsa::PagedAttention& x = job[l->many][jobs[l->many]++];
     x = a;
     const bool prefix = l == &p.prefix;
+    x.tile = l->tile;
     x.tiles = l->tiles;
     x.chunk = l->chunk;
     x.splits = l->splits;
