@@ -503,6 +503,7 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
   // the wave's own tiles: none past its last row's last key
   const int wlast = min(seen(wq0 + WQ - 1), kend), wlim0 = seen(wq0);
   const int ntw = min(nt, (wlast - k0 + BK - 1) / BK);
+  const bool busy = wq0 < sp.rows && wlast > k0;  // a wave without rows or keys only loads tiles
 
   const uint32_t rowb = static_cast<uint32_t>(a.at.kvd) * 4u;
   auto ksw = [](int r) { return HD == 64 ? (r >> 1) & 7 : r & 15; };
@@ -707,41 +708,45 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
       bn = f;
     };
     turn_over();
-    // the first tile's scores, and the reference: the max over its 64 keys
+    if (busy) {
+      // the first tile's scores, and the reference: the max over its 64 keys
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      const bf16x8_t a0 = read_k(smem, kk), a1 = read_k(smem + 32 * RB, kk);
+      for (int kk = 0; kk < KK; ++kk) {
+        const bf16x8_t a0 = read_k(smem, kk), a1 = read_k(smem + 32 * RB, kk);
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
-        sa[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, qf[qb][kk], kk == 0 ? zero : sa[qb], 0, 0, 0);
-        sb[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, qf[qb][kk], kk == 0 ? zero : sb[qb], 0, 0, 0);
+        for (int qb = 0; qb < QB; ++qb) {
+          sa[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, qf[qb][kk], kk == 0 ? zero : sa[qb], 0, 0, 0);
+          sb[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, qf[qb][kk], kk == 0 ? zero : sb[qb], 0, 0, 0);
+        }
       }
-    }
-    mask(0, sa);
-    mask(1, sb);
+      mask(0, sa);
+      mask(1, sb);
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-      mu[qb] = fmaxf(fmaxf(row_max(sa[qb]), row_max(sb[qb])) * scale_log2, -1e30f);
-    step(0, bc, 1, bp, 1, sa, sb, std::true_type());
+      for (int qb = 0; qb < QB; ++qb)
+        mu[qb] = fmaxf(fmaxf(row_max(sa[qb]), row_max(sb[qb])) * scale_log2, -1e30f);
+      step(0, bc, 1, bp, 1, sa, sb, std::true_type());
+    }
     if (nt > 2) load_tile(2, bp);
-    step(1, bn, 0, bc, 0, sb, sa, std::false_type());
+    if (busy) step(1, bn, 0, bc, 0, sb, sa, std::false_type());
     int t = 1;
-    for (; t < ntw; ++t) {
+    for (; t < (busy ? ntw : 0); ++t) {
       turn();
       step(2 * t, bc, 1, bp, 1, sa, sb, std::false_type());
       turn_over();
       if (t + 2 < nt) load_tile(t + 2, bp);
       step(2 * t + 1, bn, 0, bc, 0, sb, sa, std::false_type());
     }
+    if (busy) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        const bf16x8_t v = read_v(smem + bc * BUF + 32 * RB, k, ct);
+        for (int ct = 0; ct < CT; ++ct) {
+          const bf16x8_t v = read_v(smem + bc * BUF + 32 * RB, k, ct);
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
-          o[qb][ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[qb][k], o[qb][ct], 0, 0, 0);
-      }
+          for (int qb = 0; qb < QB; ++qb)
+            o[qb][ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[qb][k], o[qb][ct], 0, 0, 0);
+        }
+    }
     for (; t < nt; ++t) {  // the tiles of the block's later rows
       turn();
       turn_over();
@@ -756,7 +761,7 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
   // through the product with its zero probability it has, and left a NaN.
   // Where the wave's tiles hold hidden keys and its results a NaN, its rows are
   // computed again, the second product on the vector ALU, key by key.
-  if (wlim0 < min(sp.len, k0 + max(ntw, 1) * BK)) {
+  if (busy && wlim0 < min(sp.len, k0 + ntw * BK)) {
     bool odd = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
@@ -1300,8 +1305,10 @@ bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 64; }
 // The many-row kernel, whose workgroups are long and few a CU: the number whose
 // rounds over the CUs take least, with the parts' bytes. A workgroup takes 8 us
 // and 1.8 us for 64 keys of 128, or, two a CU, 2.9 of 64; parts are written
-// and read at 4 TB/s, and a join that nothing else needs is 4 us.
-int paged_chunk(bool many, int hd, int max_len, int64_t workgroups, bool joined, int* splits) {
+// and read at 4 TB/s, and a join that nothing else needs is 4 us. Where the
+// launch has `other` us of few-row work that fills the CUs between, the sum
+// counts, not the rounds.
+int paged_chunk(bool many, int hd, int max_len, int64_t workgroups, bool joined, double other, int* splits) {
   const int64_t wgs = std::max<int64_t>(workgroups, 1), cus = device_cu_count();
   const int least = many ? 256 : 512;
   const int64_t blocks = std::max(1, (max_len + least - 1) / least);
@@ -1313,7 +1320,8 @@ int paged_chunk(bool many, int hd, int max_len, int64_t workgroups, bool joined,
     for (int64_t n = 1; n <= std::min<int64_t>(blocks, 64); ++n) {
       const int64_t per = (blocks + n - 1) / n;
       const bool parts = n > 1 || joined;
-      const double us = ceil(wgs * n / slots) * (std::min<double>(per * least, max_len) * key + 8) + (parts ? n * part : 0) +
+      const double one = std::min<double>(per * least, max_len) * key + 8, rounds = wgs * n / slots;
+      const double us = (other > 0 ? std::max(one, rounds * one + other) : ceil(rounds) * one) + (parts ? n * part : 0) +
                         (parts && !joined ? 4 : 0);
       if (n == 1 || us < best) {
         best = us;

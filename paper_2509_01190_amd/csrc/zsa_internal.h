@@ -473,8 +473,9 @@ struct PagedAttention {
 };
 constexpr int kPagedManyRows = 256, kPagedFewRows = 16;  // packed rows of a workgroup (the fp32 kernel: 16 or 32)
 bool paged_matrix(int dtype, int hd);  // the bf16 matrix kernels take these heads: one for few rows, one for many
-// keys a split of up to max_len rows takes, and how many splits that makes; joined: rows have other parts anyway
-int paged_chunk(bool many, int hd, int max_len, int64_t workgroups, bool joined, int* splits);
+// keys a split of up to max_len rows takes, and how many splits that makes; joined: rows have other parts anyway; other: us of
+// few-row work beside many-row workgroups
+int paged_chunk(bool many, int hd, int max_len, int64_t workgroups, bool joined, double other, int* splits);
 int64_t paged_blocks(const PagedAttention& a, bool many);  // workgroups
 // one launch of up to two of each kind, of one type and head dim
 hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention* few, int fews,

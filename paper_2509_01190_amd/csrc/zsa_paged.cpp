@@ -114,6 +114,7 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
     const bool many = matrix && rows > kFewRows;
     most[many] = std::max(most[many], rows);
   }
+  double other = 0;  // us of the few-row work: its cached rows, half the longest each, at 5 TB/s
   auto part = [&](bool many, int64_t max_rows, int max_len, bool common) {
     Part l{};
     l.many = many;
@@ -124,7 +125,8 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
       const int64_t rows = (cu[b + 1] - cu[b]) * G;
       if (many == (matrix && rows > kFewRows)) workgroups += (rows + l.tile - 1) / l.tile;
     }
-    l.chunk = zsa::paged_chunk(many, hd, max_len, workgroups * kv.n_kv_heads, prefix > 0, &l.splits);
+    l.chunk = zsa::paged_chunk(many, hd, max_len, workgroups * kv.n_kv_heads, prefix > 0, other, &l.splits);
+    if (!many) other += workgroups * kv.n_kv_heads * hd * 2.0 * esize(kv.dtype) * max_len / 2 / 5e6;
     return l;
   };
   if (most[0] > 0) p.few = part(false, most[0], max_len, false);
