@@ -201,7 +201,7 @@ struct FewShared {  // LDS of a group of four waves
 };
 
 // the work of one of `blocks` groups of four waves, as its thread `tid`; all threads of the workgroup call it
-template <int HD>
+template <int HD, bool HEAD>
 __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, bool there, int tid, FewShared<HD>& shared) {
   constexpr int NW = FewShared<HD>::NW, KK = HD / 32, CT = HD / 16, CPR = HD / 8;
   constexpr int RB = HD * 2, HALF = 32 * RB;    // a tile of 32 rows of K, or V
@@ -218,9 +218,13 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int quarter = lane >> 4, l16 = lane & 15;
   const int row = min(i0 + l16, sp.rows - 1);  // rows past the sequence are not stored
-  const int lim = a.causal ? min(sp.first + row / a.G, sp.len) : sp.len;
-  const int lim0 = a.causal ? min(sp.first + i0 / a.G, sp.len) : sp.len;  // the tile's first row's
-  const int last = a.causal ? min(sp.first + min(i0 + 15, sp.rows - 1) / a.G, sp.len) : sp.len;
+  // A common prefix in the same job (HEAD) comes first, filled up to whole steps: key
+  // j below `head` is its row j, key j from there on row j - head of the
+  // sequence's own
+  const int head = HEAD ? (a.head_len + 31) & ~31 : 0, end = head + sp.len;
+  auto seen = [&](int i) { return head + (a.causal ? max(min(sp.first + i / a.G, sp.len), 0) : sp.len); };
+  const int lim = seen(row), lim0 = seen(i0);  // a lane's keys are those below lim; the tile's first row's
+  const int last = seen(min(i0 + 15, sp.rows - 1));
   const int k0 = split * a.chunk, kend = live ? min(last, k0 + a.chunk) : 0;
   const float scale_log2 = a.scale * kLog2e;
 
@@ -237,20 +241,23 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
   }
   unsigned char* mine = smem + wave * (2 * HALF);
   const uint32_t lds0 = lds_address(smem) + wave * (2 * HALF);
-  const scalar_ids table = scalar(sp.table);
+  const scalar_ids table = scalar(sp.table), head_table = scalar(a.head_table);
   const char* pool = static_cast<const char*>(a.at.pool);
   // 16 rows from row j on, of page `page` (-1 where the sequence has ended): `col` bytes into a row
   auto resource = [&](int j, int page, uint32_t col) {
     const bool there = page >= 0 && page < a.at.n_pages;
-    const uint32_t bytes = there ? static_cast<uint32_t>(min(sp.len - j, 16)) * rowb - col : 0u;
+    const uint32_t bytes = there ? static_cast<uint32_t>(min((HEAD && j < head ? a.head_len : end) - j, 16)) * rowb - col : 0u;
     u32x4 res = buffer_resource(pool + (there ? page : 0) * (a.at.page_stride * 2) +
-                                    static_cast<uint32_t>(j & ((1 << a.at.shift) - 1)) * rowb + col,
+                                    static_cast<uint32_t>((HEAD && j >= head ? j - head : j) & ((1 << a.at.shift) - 1)) * rowb + col,
                                 bytes);
     // a load in asm may follow a vector instruction's write of its scalar operands by five states at least
     asm volatile("s_nop 4" : "+s"(res));
     return res;
   };
-  auto page_of = [&](int j) { return j < sp.len ? table[j >> a.at.shift] : -1; };
+  auto page_of = [&](int j) {
+    if (HEAD && j < head) return j < a.head_len ? head_table[j >> a.at.shift] : -1;
+    return j < end ? table[(j - head) >> a.at.shift] : -1;
+  };
   const uint32_t kcol = g * RB, vcol = rowb / 2 + g * RB;
   auto load = [&](int j0, int pg0, int pg1, uint32_t lds, uint32_t col, const uint32_t (&off)[NL]) {
 #pragma unroll
@@ -269,7 +276,12 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
   // fragment addresses: a transposing read gives group `quarter` of 16 lanes
   // the keys 4 quarter .. + 3 of 16 channels, one a lane
   const uint32_t vrow = 4 * quarter + (l16 >> 2);
-  const int ks0 = ksw(l16), vs0 = vsw(vrow);
+  uint32_t kaddr[KK], vaddr[CT];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) kaddr[kk] = l16 * RB + (((4 * kk + quarter) ^ ksw(l16)) << 4);
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+    vaddr[ct] = HALF + vrow * RB + (lane & 1) * 8 + (((2 * ct + ((lane >> 1) & 1)) ^ vsw(vrow)) << 4);
 
   int j0 = k0 + wave * 32;
   int pg0 = page_of(j0), pg1 = page_of(j0 + 16);
@@ -277,6 +289,8 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
     load(j0, pg0, pg1, lds0, kcol, koff);
     load(j0, pg0, pg1, lds0 + HALF, vcol, voff);
   }
+  int nx0 = page_of(j0 + 32 * NW), nx1 = page_of(j0 + 32 * NW + 16);  // read a step before the loads that need them
+  asm volatile("" : "+s"(nx0), "+s"(nx1));
   bf16x8_t qf[KK];
   if (j0 < kend) {
     const bf16_t* qp = static_cast<const bf16_t*>(a.q) + static_cast<int64_t>(sp.lo + row / a.G) * a.q_stride +
@@ -291,29 +305,36 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
   for (; j0 < kend; j0 += 32 * NW) {
     const int jn = j0 + 32 * NW;
     const bool more = jn < kend;
-    pg0 = page_of(jn);
-    pg1 = page_of(jn + 16);
+    pg0 = nx0;
+    pg1 = nx1;
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // K is here, V may be under way
     __builtin_amdgcn_sched_barrier(0);
     f32x4_t s[2];
+    bf16x8_t kf[KK][2];  // all read before the products: one latency, not one a product
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const bf16x8_t k = __builtin_bit_cast(
-            bf16x8_t, *reinterpret_cast<const u32x4*>(mine + (16 * t + l16) * RB + (((4 * kk + quarter) ^ ks0) << 4)));
-        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[kk], kk == 0 ? zero : s[t], 0, 0, 0);
-      }
+      for (int t = 0; t < 2; ++t)
+        kf[kk][t] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(mine + kaddr[kk] + 16 * t * RB));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kk][t], qf[kk], kk == 0 ? zero : s[t], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) load(jn, pg0, pg1, lds0, kcol, koff);
+    nx0 = page_of(jn + 32 * NW);
+    nx1 = page_of(jn + 32 * NW + 16);
     // s[t][r]: key j0 + 16 t + 4 quarter + r, packed row `row`
-    if (j0 + 32 > lim0) {
+    if (j0 + 32 > (HEAD && j0 < head ? a.head_len : lim0)) {
+      const int left = (HEAD && j0 < head ? a.head_len : lim) - j0;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (j0 + 16 * t + 4 * quarter + r >= lim) s[t][r] = -INFINITY;
+          if (16 * t + 4 * quarter + r >= left) s[t][r] = -INFINITY;
     }
     const float mloc = quarter_swap_max(fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                                               fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))));
@@ -347,12 +368,13 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // V is here, the next K may be under way
     else
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("" : "+s"(nx0), "+s"(nx1));  // here: scalar loads under way make every wait for LDS one for all
     __builtin_amdgcn_sched_barrier(0);
     // A value that is not finite must not reach a row that does not see its
     // key, through the product with its zero probability: where the tile holds
     // hidden keys and such values, it goes through the vector ALU, key by key.
     bool odd = false;
-    if (lim0 < min(j0 + 32, sp.len)) {
+    if ((!HEAD || j0 >= head) && lim0 < min(j0 + 32, end)) {
 #pragma unroll
       for (int i = 0; i < 2 * NL; ++i) {
         const u32x4 w = *reinterpret_cast<const u32x4*>(mine + HALF + i * 1024 + lane * 16);
@@ -363,13 +385,17 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
       odd = __builtin_amdgcn_ballot_w64(odd) != 0;
     }
     if (!odd) {
+      bf16x8_t vf[CT];
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        const unsigned char* vr = mine + HALF + vrow * RB + (lane & 1) * 8 + (((2 * ct + ((lane >> 1) & 1)) ^ vs0) << 4);
-        const bf16x8_t v = __builtin_bit_cast(bf16x8_t, lds_read_columns(vr, vr + 16 * RB));
-        o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, hi), o[ct], 0, 0, 0);
-        o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, lo), o[ct], 0, 0, 0);
-      }
+      for (int ct = 0; ct < CT; ++ct)
+        vf[ct] = __builtin_bit_cast(bf16x8_t, lds_read_columns(mine + vaddr[ct], mine + vaddr[ct] + 16 * RB));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+        o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[ct], __builtin_bit_cast(bf16x8_t, hi), o[ct], 0, 0, 0);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+        o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[ct], __builtin_bit_cast(bf16x8_t, lo), o[ct], 0, 0, 0);
     } else {
 #pragma unroll
       for (int kk = 0; kk < 32; ++kk) {
@@ -442,13 +468,13 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
   }
 }
 
-template <int HD>
+template <int HD, bool HEAD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2))) void paged_few_kernel(
     PagedJobs jobs) {
   __shared__ __align__(1024) FewShared<HD> shared;
   const int which = blockIdx.x >= jobs.first;
   const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
-  few_rows<HD>(a, blockIdx.x - (which ? jobs.first : 0), true, threadIdx.x, shared);
+  few_rows<HD, HEAD>(a, blockIdx.x - (which ? jobs.first : 0), true, threadIdx.x, shared);
 }
 
 // bf16, heads of 64 and 128, many packed rows: bound by the products. A
@@ -908,7 +934,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const uint32_t block = (blockIdx.x - many.blocks) * GROUPS + group;
     const int which = block >= few.first;
     const PagedAttention a = few.job[which];
-    few_rows<HD>(a, block - (which ? few.first : 0), block < few.blocks, threadIdx.x & 255, shared.few[group]);
+    few_rows<HD, false>(a, block - (which ? few.first : 0), block < few.blocks, threadIdx.x & 255, shared.few[group]);
   }
 }
 
@@ -925,7 +951,7 @@ struct F32Shared {
   float m[NW][W], l[NW][W];
 };
 
-template <typename T, int HD, int W>
+template <typename T, int HD, int W, bool HEAD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 1 : HD == 64 ? 2 : 3))) void paged_f32_kernel(
     PagedJobs jobs) {
   constexpr int NW = 4, E = sizeof(T);
@@ -950,9 +976,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = lane / W, col = lane % W;
   const int row = min(i0 + col, sp.rows - 1);  // rows past the sequence are not stored
-  const int lim = a.causal ? min(sp.first + row / a.G, sp.len) : sp.len;
-  const int lim0 = a.causal ? min(sp.first + i0 / a.G, sp.len) : sp.len;  // the tile's first row's
-  const int last = a.causal ? min(sp.first + min(i0 + W - 1, sp.rows - 1) / a.G, sp.len) : sp.len;
+  // A common prefix in the same job (HEAD) comes first, filled up to whole steps: key
+  // j below `head` is its row j, key j from there on row j - head of the
+  // sequence's own
+  const int head = HEAD ? (a.head_len + 31) & ~31 : 0, end = head + sp.len;
+  auto seen = [&](int i) { return head + (a.causal ? max(min(sp.first + i / a.G, sp.len), 0) : sp.len); };
+  const int lim = seen(row), lim0 = seen(i0);  // a lane's keys are those below lim; the tile's first row's
+  const int last = seen(min(i0 + W - 1, sp.rows - 1));
   const int k0 = split * a.chunk, kend = min(last, k0 + a.chunk);
 
   // K row r of a tile keeps its 16-byte chunk c at c ^ ksw(r): the rows of a
@@ -970,20 +1000,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
   }
   unsigned char* mine = smem + wave * (2 * HALF);
   const uint32_t lds0 = lds_address(smem) + wave * (2 * HALF);
-  const scalar_ids table = scalar(sp.table);
+  const scalar_ids table = scalar(sp.table), head_table = scalar(a.head_table);
   const char* pool = static_cast<const char*>(a.at.pool);
   // 16 rows from row j on, of page `page` (-1 where the sequence has ended): `col` bytes into a row
   auto resource = [&](int j, int page, uint32_t col) {
     const bool there = page >= 0 && page < a.at.n_pages;
-    const uint32_t bytes = there ? static_cast<uint32_t>(min(sp.len - j, 16)) * rowb - col : 0u;
+    const uint32_t bytes = there ? static_cast<uint32_t>(min((HEAD && j < head ? a.head_len : end) - j, 16)) * rowb - col : 0u;
     u32x4 res = buffer_resource(pool + (there ? page : 0) * (a.at.page_stride * E) +
-                                    static_cast<uint32_t>(j & ((1 << a.at.shift) - 1)) * rowb + col,
+                                    static_cast<uint32_t>((HEAD && j >= head ? j - head : j) & ((1 << a.at.shift) - 1)) * rowb + col,
                                 bytes);
     // a load in asm may follow a vector instruction's write of its scalar operands by five states at least
     asm volatile("s_nop 4" : "+s"(res));
     return res;
   };
-  auto page_of = [&](int j) { return j < sp.len ? table[j >> a.at.shift] : -1; };
+  auto page_of = [&](int j) {
+    if (HEAD && j < head) return j < a.head_len ? head_table[j >> a.at.shift] : -1;
+    return j < end ? table[(j - head) >> a.at.shift] : -1;
+  };
   const uint32_t kcol = g * RB, vcol = rowb / 2 + g * RB;
   auto load = [&](int j0, int pg0, int pg1, uint32_t lds, uint32_t col, const uint32_t (&off)[NL]) {
 #pragma unroll
@@ -1003,6 +1036,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
   const bool vch = HD >= W || col < HD;  // lanes whose channel exists
   // the key of register r of tile t; the same of the channel of a register of O
   auto key = [&](int t, int r) { return t * W + 8 * (r >> 2) + 4 * group + (r & 3); };
+  // fragment addresses: the lane's four channels of K row col, its channel of V
+  // row 4 group, whose chunks are those of all its rows (vsw)
+  uint32_t kaddr[KK], vaddr[CT];
+#pragma unroll
+  for (int c = 0; c < KK; ++c) {
+    const int ch = 4 * (NG * c + group) * E;
+    kaddr[c] = col * RB + (((ch >> 4) ^ ksw(col)) << 4) + (ch & 15);
+  }
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int ch = (ct * W + (HD < W ? col % HD : col)) * E;
+    vaddr[ct] = HALF + 4 * group * RB + (((ch >> 4) ^ vsw(4 * group)) << 4) + (ch & 15);
+  }
   auto mfma = [](float x, float y, acc_t c) {
     if constexpr (W == 32) return __builtin_amdgcn_mfma_f32_32x32x2f32(x, y, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x4f32(x, y, c, 0, 0, 0);
@@ -1013,6 +1059,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
     load(j0, pg0, pg1, lds0, kcol, koff);
     load(j0, pg0, pg1, lds0 + HALF, vcol, voff);
   }
+  int nx0 = page_of(j0 + 32 * NW), nx1 = page_of(j0 + 32 * NW + 16);  // read a step before the loads that need them
+  asm volatile("" : "+s"(nx0), "+s"(nx1));
   float4 qf[KK];
   if (j0 < kend) {
     const T* qp = static_cast<const T*>(a.q) + static_cast<int64_t>(sp.lo + row / a.G) * a.q_stride + (g * a.G + row % a.G) * HD;
@@ -1025,32 +1073,41 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
   for (; j0 < kend; j0 += 32 * NW) {
     const int jn = j0 + 32 * NW;
     const bool more = jn < kend;
-    pg0 = page_of(jn);
-    pg1 = page_of(jn + 16);
+    pg0 = nx0;
+    pg1 = nx1;
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // K is here, V may be under way
     __builtin_amdgcn_sched_barrier(0);
     acc_t s[NT];
+    float4 kf[KK][NT];  // all read before the products: one latency, not one a product
 #pragma unroll
     for (int c = 0; c < KK; ++c)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const int kr = t * W + col, ch = 4 * (NG * c + group) * E;  // byte of the lane's four channels in a row
-        const float4 k4 = load4<T>(reinterpret_cast<const T*>(mine + kr * RB + (((ch >> 4) ^ ksw(kr)) << 4) + (ch & 15)));
-        s[t] = mfma(k4.x, qf[c].x, c == 0 ? zero : s[t]);
-        s[t] = mfma(k4.y, qf[c].y, s[t]);
-        s[t] = mfma(k4.z, qf[c].z, s[t]);
-        s[t] = mfma(k4.w, qf[c].w, s[t]);
-      }
+      for (int t = 0; t < NT; ++t) kf[c][t] = load4<T>(reinterpret_cast<const T*>(mine + kaddr[c] + t * W * RB));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int c = 0; c < KK; ++c) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[t] = mfma(kf[c][t].x, qf[c].x, c == 0 ? zero : s[t]);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[t] = mfma(kf[c][t].y, qf[c].y, s[t]);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[t] = mfma(kf[c][t].z, qf[c].z, s[t]);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[t] = mfma(kf[c][t].w, qf[c].w, s[t]);
+    }
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) load(jn, pg0, pg1, lds0, kcol, koff);
-    const bool edge = j0 + 32 > lim0;
+    nx0 = page_of(jn + 32 * NW);
+    nx1 = page_of(jn + 32 * NW + 16);
+    const bool edge = j0 + 32 > (HEAD && j0 < head ? a.head_len : lim0);
+    const int left = (HEAD && j0 < head ? a.head_len : lim) - j0;
     float mloc = -INFINITY;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
-        s[t][r] = edge && j0 + key(t, r) >= lim ? -INFINITY : s[t][r] * a.scale;
+        s[t][r] = edge && key(t, r) >= left ? -INFINITY : s[t][r] * a.scale;
         mloc = fmaxf(mloc, s[t][r]);
       }
     mloc = W == 32 ? half_swap_max(mloc) : quarter_swap_max(mloc);
@@ -1076,10 +1133,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");  // V is here, the next K may be under way
     else
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("" : "+s"(nx0), "+s"(nx1));  // here: scalar loads under way make every wait for LDS one for all
     __builtin_amdgcn_sched_barrier(0);
     // hidden keys' values that are not finite: key by key (few_rows)
     bool odd = false;
-    if (lim0 < min(j0 + 32, sp.len)) {
+    if ((!HEAD || j0 >= head) && lim0 < min(j0 + 32, end)) {
 #pragma unroll
       for (int i = 0; i < HALF / 1024; ++i) {
         const u32x4 w = *reinterpret_cast<const u32x4*>(mine + HALF + i * 1024 + lane * 16);
@@ -1093,14 +1151,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          const int jj = key(t, r);
+        for (int r0 = 0; r0 < NR; r0 += 4) {
+          float vf[4][CT];
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            const int ch = (ct * W + (HD < W ? col % HD : col)) * E;
-            const float v = to_f32(*reinterpret_cast<const T*>(mine + HALF + jj * RB + (((ch >> 4) ^ vsw(jj)) << 4) + (ch & 15)));
-            o[ct] = mfma(vch ? v : 0.f, s[t][r], o[ct]);
-          }
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+              vf[r][ct] = to_f32(*reinterpret_cast<const T*>(mine + vaddr[ct] + (t * W + 2 * r0 + r) * RB));
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[ct] = mfma(vch ? vf[r][ct] : 0.f, s[t][r0 + r], o[ct]);
         }
     } else {
 #pragma unroll
@@ -1252,19 +1313,31 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restric
     lse[static_cast<int64_t>(h) * Trows + t] = L == 0.f ? -INFINITY : LOG2 ? (M + log2f(L)) * kLn2 : M + logf(L);
 }
 
-template <typename T, int W>
+template <typename T, int W, bool HEAD>
 hipError_t f32_dispatch(hipStream_t s, const PagedJobs& jobs, dim3 g) {
   const dim3 block(256);
   switch (jobs.job[0].hd) {
-    case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16, W>, g, block, 0, s, jobs);
-    case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32, W>, g, block, 0, s, jobs);
+    case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16, W, HEAD>, g, block, 0, s, jobs);
+    case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32, W, HEAD>, g, block, 0, s, jobs);
     default: break;
   }
   if constexpr (sizeof(T) == 4) {
-    if (jobs.job[0].hd == 64) return launch(K_ATTENTION, paged_f32_kernel<T, 64, W>, g, block, 0, s, jobs);
-    if (jobs.job[0].hd == 128) return launch(K_ATTENTION, paged_f32_kernel<T, 128, W>, g, block, 0, s, jobs);
+    if (jobs.job[0].hd == 64) return launch(K_ATTENTION, paged_f32_kernel<T, 64, W, HEAD>, g, block, 0, s, jobs);
+    if (jobs.job[0].hd == 128) return launch(K_ATTENTION, paged_f32_kernel<T, 128, W, HEAD>, g, block, 0, s, jobs);
   }
   return hipErrorInvalidValue;
+}
+
+template <bool HEAD>
+hipError_t few_dispatch(hipStream_t s, int dtype, const PagedJobs& jobs) {
+  const dim3 g(jobs.blocks);
+  const PagedAttention& a = jobs.job[0];
+  if (paged_matrix(dtype, a.hd)) {
+    if (a.hd == 64) return launch(K_ATTENTION, paged_few_kernel<64, HEAD>, g, dim3(256), 0, s, jobs);
+    return launch(K_ATTENTION, paged_few_kernel<128, HEAD>, g, dim3(256), 0, s, jobs);
+  }
+  if (a.tile == 32) return dtype == 1 ? f32_dispatch<bf16_t, 32, HEAD>(s, jobs, g) : f32_dispatch<float, 32, HEAD>(s, jobs, g);
+  return dtype == 1 ? f32_dispatch<bf16_t, 16, HEAD>(s, jobs, g) : f32_dispatch<float, 16, HEAD>(s, jobs, g);
 }
 
 template <typename T>
@@ -1300,19 +1373,21 @@ hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a) {
 bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 64; }
 
 // Splits of the keys. The few-row kernels: enough workgroups for four a CU, of
-// 512 keys at least: a second split needs the parts joined, which takes as long
-// (4 sequences of up to 300 rows, 12 heads of 64: 10.9 us, in splits of 128 14.9).
+// 512 keys at least, and in bf16 one for 1024: a second split needs the parts
+// joined. One split / two, us: 4 sequences of up to 1000 rows, 12 heads of 64,
+// 11.0 / 14.6; 1 of 1000, 32 heads of 128 on 8, 12.1 / 14.3; 4 of 2000 16.6 / 14.3;
+// fp32, 1 of 1000, 12 heads of 64, 19.8 / 15.2.
 // The many-row kernel, whose workgroups are long and few a CU: the number whose
 // rounds over the CUs take least, with the parts' bytes. A workgroup takes 8 us
 // and 1.8 us for 64 keys of 128, or, two a CU, 2.9 of 64; parts are written
 // and read at 4 TB/s, and a join that nothing else needs is 4 us. Where the
 // launch has `other` us of few-row work that fills the CUs between, the sum
 // counts, not the rounds.
-int paged_chunk(bool many, int hd, int max_len, int64_t workgroups, bool joined, double other, int* splits) {
+int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, bool joined, double other, int* splits) {
   const int64_t wgs = std::max<int64_t>(workgroups, 1), cus = device_cu_count();
   const int least = many ? 256 : 512;
   const int64_t blocks = std::max(1, (max_len + least - 1) / least);
-  int64_t want = std::min(blocks, std::max<int64_t>(1, (4 * cus + wgs - 1) / wgs));
+  int64_t want = matrix && max_len <= 1024 ? 1 : std::min(blocks, std::max<int64_t>(1, (4 * cus + wgs - 1) / wgs));
   if (many) {
     const double slots = (hd == 64 ? 2.0 : 1.0) * std::max<int64_t>(cus, 1), key = (hd == 64 ? 2.9 : 1.8) / 64;
     const double part = static_cast<double>(wgs) * kPagedManyRows * hd * 8 / 4e6;
@@ -1357,13 +1432,7 @@ hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention
       return launch(K_ATTENTION, paged_many_kernel<64, 2, 4>, dim3(w[1].blocks + w[0].blocks), dim3(256), 0, s, w[1], w[0]);
     return launch(K_ATTENTION, paged_many_kernel<128, 1, 8>, dim3(w[1].blocks + (w[0].blocks + 1) / 2), dim3(512), 0, s, w[1], w[0]);
   }
-  const dim3 g(w[0].blocks);
-  if (paged_matrix(dtype, hd)) {
-    if (hd == 64) return launch(K_ATTENTION, paged_few_kernel<64>, g, dim3(256), 0, s, w[0]);
-    return launch(K_ATTENTION, paged_few_kernel<128>, g, dim3(256), 0, s, w[0]);
-  }
-  if (few[0].tile == 32) return dtype == 1 ? f32_dispatch<bf16_t, 32>(s, w[0], g) : f32_dispatch<float, 32>(s, w[0], g);
-  return dtype == 1 ? f32_dispatch<bf16_t, 16>(s, w[0], g) : f32_dispatch<float, 16>(s, w[0], g);
+  return few[0].head_len > 0 ? few_dispatch<true>(s, dtype, w[0]) : few_dispatch<false>(s, dtype, w[0]);
 }
 
 hipError_t launch_paged_join(hipStream_t s, int dtype, const float2* ml, const float* o, int parts, int T, int H,

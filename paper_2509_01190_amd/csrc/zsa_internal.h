@@ -457,6 +457,8 @@ struct PagedAttention {
   const int32_t* cu;          // null: all T rows are one sequence's (a common prefix)
   const int32_t* kv_len;      // null: max_len rows
   int max_len;                // rows from this one on are not read
+  const int32_t* head_table;  // pages of a common prefix that the few-row kernels put before the rows, and
+  int head_len;               // its rows (0: none)
   int T, B, H, G, hd;
   int causal;
   float scale;
@@ -475,7 +477,7 @@ constexpr int kPagedManyRows = 256, kPagedFewRows = 16;  // packed rows of a wor
 bool paged_matrix(int dtype, int hd);  // the bf16 matrix kernels take these heads: one for few rows, one for many
 // keys a split of up to max_len rows takes, and how many splits that makes; joined: rows have other parts anyway; other: us of
 // few-row work beside many-row workgroups
-int paged_chunk(bool many, int hd, int max_len, int64_t workgroups, bool joined, double other, int* splits);
+int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, bool joined, double other, int* splits);
 int64_t paged_blocks(const PagedAttention& a, bool many);  // workgroups
 // one launch of up to two of each kind, of one type and head dim
 hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention* few, int fews,

@@ -143,6 +143,23 @@ def test_common_prefix(dtype, H, kv, hd, prefix, new):
     Batch(dtype, H, kv, hd, 32, new, [max(n, 0) for n in lens], prefix, seed=prefix).check(True)
 
 
+@pytest.mark.parametrize("dtype,H,kv,hd,prefix,batch,n", [
+    ("bf16", 16, 8, 128, 521, 17, 1),    # one row a sequence, 34 packed rows a head over the prefix
+    ("bf16", 8, 8, 128, 521, 17, 1),     # 17: few enough for the few-row kernel there too
+    ("bf16", 8, 8, 128, 521, 17, 3),
+    ("bf16", 16, 16, 64, 1100, 18, 40),
+    ("f32", 8, 8, 128, 530, 9, 1),
+    ("f32", 16, 8, 128, 530, 9, 3),
+    ("f32", 16, 16, 64, 530, 9, 20),
+])
+def test_long_prefix_of_many_sequences(dtype, H, kv, hd, prefix, batch, n):
+    # more than 32 MB if every sequence read it: rows of its own in the call's parts
+    new = [n if b % 3 else 1 for b in range(batch)]
+    lens = [m + (11 * b) % 70 for b, m in enumerate(new)]
+    lens[4] = 0
+    Batch(dtype, H, kv, hd, 16, new, lens, prefix, seed=prefix + n).check(True)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prefix_equals_the_same_rows_repeated(dtype):
     # the prefix cached once, against every sequence holding it as its own rows

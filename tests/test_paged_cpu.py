@@ -78,9 +78,10 @@ def test_appends_that_are_refused(kw, code):
     (dict(dev=None), zsa.EINVAL), (dict(offs=(0, 2, 1)), zsa.ESHAPE), (dict(most=-1), zsa.EINVAL),
     (dict(most=65), zsa.ESHAPE),                                                 # beyond the table
     (dict(prefix=-1), zsa.EINVAL), (dict(prefix=20), zsa.EINVAL),                # no prefix pages
-    (dict(prefix=20, pages=PTR[7]), zsa.EINVAL),                                 # parts, and no workspace
-    (dict(prefix=20, pages=PTR[7], ws=PTR[8], wsb=64), zsa.EWORKSPACE),
-    (dict(prefix=20, pages=PTR[7], ws=ODD, wsb=1 << 30), zsa.EALIGN),
+    (dict(prefix=40000, pages=PTR[7]), zsa.EINVAL),                              # parts, and no workspace
+    (dict(prefix=40000, pages=PTR[7], ws=PTR[8], wsb=64), zsa.EWORKSPACE),
+    (dict(prefix=40000, pages=PTR[7], ws=ODD, wsb=1 << 30), zsa.EALIGN),
+    (dict(prefix=(1 << 30) + 1, pages=PTR[7]), zsa.EUNSUPPORTED),
     (dict(offs=(0, 1 << 30), H=2, qs=128, os=128, lse=PTR[3]), zsa.EUNSUPPORTED),
 ])
 def test_attentions_that_are_refused(kw, code):
@@ -99,10 +100,11 @@ def test_workspace_is_that_of_the_parts():
     h = cu(0, 1, 3)
     size = zsa.lib().zsa_paged_attention_workspace_size
     assert size(ctypes.byref(c), 4, 2, zsa._hp32(h), 64, 0) == 0                 # one part: written at once
-    two = size(ctypes.byref(c), 4, 2, zsa._hp32(h), 64, 20)
+    assert size(ctypes.byref(c), 4, 2, zsa._hp32(h), 64, 20) == 0                # a short prefix is read with the rows' own
+    two = size(ctypes.byref(c), 4, 2, zsa._hp32(h), 64, 40000)
     assert two >= 2 * 3 * 4 * (2 + 64) * 4                                       # the prefix's part and the rows' own
-    assert size(None, 4, 2, zsa._hp32(h), 64, 20) == 0
-    assert size(ctypes.byref(c), 4, 2, zsa._hp32(cu(0, 0, 0)), 64, 20) == 0
+    assert size(None, 4, 2, zsa._hp32(h), 64, 40000) == 0
+    assert size(ctypes.byref(c), 4, 2, zsa._hp32(cu(0, 0, 0)), 64, 40000) == 0
 
 
 # ---------------------------------------------------------------------------- the oracle
