@@ -254,9 +254,12 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
     asm volatile("s_nop 4" : "+s"(res));
     return res;
   };
+  // (the read does not wait for the length: up to the table's end it goes through)
   auto page_of = [&](int j) {
-    if (HEAD && j < head) return j < a.head_len ? head_table[j >> a.at.shift] : -1;
-    return j < end ? table[(j - head) >> a.at.shift] : -1;
+    const bool first = HEAD && j < head;
+    const int p = (first ? j : j - head) >> a.at.shift, most = first ? (a.head_len - 1) >> a.at.shift : a.at.max_pages - 1;
+    const int page = most >= 0 ? (first ? head_table : table)[min(p, most)] : -1;
+    return j < (first ? a.head_len : end) ? page : -1;
   };
   const uint32_t kcol = g * RB, vcol = rowb / 2 + g * RB;
   auto load = [&](int j0, int pg0, int pg1, uint32_t lds, uint32_t col, const uint32_t (&off)[NL]) {
@@ -540,10 +543,11 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
   const uint32_t lds0 = lds_address(smem) + wave * 1024;
   const char* pool = static_cast<const char*>(a.at.pool);
   // ids of the 64 pages from `idp` on, one a lane, and of the 64 after them
-  const int most = sp.len > 0 ? (sp.len - 1) >> a.at.shift : 0;
+  // (the reads do not wait for the length: up to the table's end they go through)
+  const int most = a.at.max_pages - 1;
   int idp = k0 >> a.at.shift;
-  auto read_ids = [&](int from) { return sp.len > 0 ? sp.table[min(from + lane, most)] : -1; };
-  int ids = nt > 0 ? read_ids(idp) : -1, idn = nt > 0 ? read_ids(idp + 64) : -1;
+  auto read_ids = [&](int from) { return most >= 0 ? sp.table[min(from + lane, most)] : -1; };
+  int ids = read_ids(idp), idn = read_ids(idp + 64);
   auto load_rows = [&](int j, uint32_t lds) {  // K and V of RPL rows from row j on
     const int p = j >> a.at.shift;
     if (p >= idp + 64) {
@@ -1013,9 +1017,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ?
     asm volatile("s_nop 4" : "+s"(res));
     return res;
   };
+  // (the read does not wait for the length: up to the table's end it goes through)
   auto page_of = [&](int j) {
-    if (HEAD && j < head) return j < a.head_len ? head_table[j >> a.at.shift] : -1;
-    return j < end ? table[(j - head) >> a.at.shift] : -1;
+    const bool first = HEAD && j < head;
+    const int p = (first ? j : j - head) >> a.at.shift, most = first ? (a.head_len - 1) >> a.at.shift : a.at.max_pages - 1;
+    const int page = most >= 0 ? (first ? head_table : table)[min(p, most)] : -1;
+    return j < (first ? a.head_len : end) ? page : -1;
   };
   const uint32_t kcol = g * RB, vcol = rowb / 2 + g * RB;
   auto load = [&](int j0, int pg0, int pg1, uint32_t lds, uint32_t col, const uint32_t (&off)[NL]) {
@@ -1373,10 +1380,10 @@ hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a) {
 bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 64; }
 
 // Splits of the keys. The few-row kernels: enough workgroups for four a CU, of
-// 512 keys at least, and in bf16 one for 1024: a second split needs the parts
+// 512 keys at least, and one for 1024 in bf16 or where they fill half the CUs: a second split needs the parts
 // joined. One split / two, us: 4 sequences of up to 1000 rows, 12 heads of 64,
 // 11.0 / 14.6; 1 of 1000, 32 heads of 128 on 8, 12.1 / 14.3; 4 of 2000 16.6 / 14.3;
-// fp32, 1 of 1000, 12 heads of 64, 19.8 / 15.2.
+// fp32, 1 of 1000, 12 heads of 64, 19.8 / 15.2, 16 of up to 1024 21.0 / 21.6.
 // The many-row kernel, whose workgroups are long and few a CU: the number whose
 // rounds over the CUs take least, with the parts' bytes. A workgroup takes 8 us
 // and 1.8 us for 64 keys of 128, or, two a CU, 2.9 of 64; parts are written
@@ -1387,7 +1394,7 @@ int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups,
   const int64_t wgs = std::max<int64_t>(workgroups, 1), cus = device_cu_count();
   const int least = many ? 256 : 512;
   const int64_t blocks = std::max(1, (max_len + least - 1) / least);
-  int64_t want = matrix && max_len <= 1024 ? 1 : std::min(blocks, std::max<int64_t>(1, (4 * cus + wgs - 1) / wgs));
+  int64_t want = max_len <= 1024 && (matrix || 2 * wgs >= cus) ? 1 : std::min(blocks, std::max<int64_t>(1, (4 * cus + wgs - 1) / wgs));
   if (many) {
     const double slots = (hd == 64 ? 2.0 : 1.0) * std::max<int64_t>(cus, 1), key = (hd == 64 ? 2.9 : 1.8) / 64;
     const double part = static_cast<double>(wgs) * kPagedManyRows * hd * 8 / 4e6;
