@@ -458,7 +458,8 @@ int zsa_paged_append(void* stream, const zsa_paged_kv* kv, const void* k, int64_
  *   out      [T, n_heads*head_dim], row stride out_stride; lse [n_heads, T]
  *            fp32 or NULL
  *   ws >= zsa_paged_attention_workspace_size(..., prefix_len 0)
- * bf16 or fp32, sums and softmax in fp32; head_dim 16, 32, 64 or 128.
+ * bf16 or fp32, sums and softmax in fp32; head_dim 16, 32, 64 or 128. Up to
+ * 2^30 rows times heads, and 2^30 cached rows a sequence.
  */
 int zsa_paged_attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride,
                         int32_t n_heads, int32_t causal, float scale, int32_t batch,

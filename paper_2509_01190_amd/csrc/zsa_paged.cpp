@@ -174,8 +174,8 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
                      kv->page_size);
   if (max_kv_len > (1 << 30) || prefix_len > (1 << 30))
     return set_error(ZSA_EUNSUPPORTED, "max_kv_len %d, prefix_len %d beyond 2^30", max_kv_len, prefix_len);
-  if (static_cast<int64_t>(T) * n_heads >= (int64_t{1} << 31))
-    return set_error(ZSA_EUNSUPPORTED, "%d rows of %d heads: 2^31 or more", T, n_heads);
+  if (static_cast<int64_t>(T) * n_heads >= (int64_t{1} << 30))
+    return set_error(ZSA_EUNSUPPORTED, "%d rows of %d heads: 2^30 or more", T, n_heads);
   const size_t need = zsa_paged_attention_workspace_size(kv, n_heads, batch, cu_host, max_kv_len, prefix_len);
   if (need > 0) {
     CHECK(check_ptr16(ws, "ws"));
@@ -207,6 +207,7 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
   // the work of the few-row kernel and of the many-row one
   zsa::PagedAttention job[2][2];
   int jobs[2] = {0, 0};
+  int64_t threads = 0;
   for (const Part* l : {&p.prefix, &p.few, &p.many}) {
     if (l->splits == 0) continue;
     zsa::PagedAttention& x = job[l->many][jobs[l->many]++];
@@ -237,10 +238,11 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
       x.ml = ml + (prefix ? 0 : p.prefix.splits) * rows;
       x.o = o + (prefix ? 0 : p.prefix.splits) * rows * kv->head_dim;
     }
-    if (zsa::paged_blocks(x, l->many) > (1 << 22))
-      return set_error(ZSA_EUNSUPPORTED, "%d sequences of up to %d rows of %d heads: more workgroups than a grid holds",
-                       batch, max_new, n_heads);
+    threads += zsa::paged_blocks(x, l->many) * (l->many && kv->head_dim == 128 ? 512 : 256);
   }
+  if (threads >= (int64_t{1} << 32) - 512)  // (what a grid holds)
+    return set_error(ZSA_EUNSUPPORTED, "%d sequences of up to %d rows of %d heads: more workgroups than a grid holds",
+                     batch, max_new, n_heads);
   HIP_TRY(zsa::launch_paged_attention(s, kv->dtype, job[0], jobs[0], job[1], jobs[1]), "paged attention");
   if (p.join())
     HIP_TRY(zsa::launch_paged_join(s, kv->dtype, ml, o, p.parts(), T, n_heads, kv->head_dim, out, out_stride, lse),

@@ -9,6 +9,7 @@ else.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -419,16 +420,19 @@ def _rows_stride(kv: PagedKV, rows: torch.Tensor, total: int, cols: int, what: s
     return stride if total > 1 else cols
 
 
-def _on(index: int, call, *args) -> None:
-    """A C entry point on a device, on its current stream. (torch.cuda.device
-    and torch.cuda.current_stream take 3 us, these 0.3.)"""
-    if torch._C._cuda_getDevice() == index:
-        _check(call(torch._C._cuda_getCurrentRawStream(index), *args))
-    else:
-        with torch.cuda.device(index):
-            _check(call(torch._C._cuda_getCurrentRawStream(index), *args))
+def _on_its_device(fn):
+    """The call with the cache's device current, whichever is."""
+    @functools.wraps(fn)
+    def call(*args, **kw):
+        kv = kw["kv"] if "kv" in kw else args[0] if isinstance(args[0], PagedKV) else args[1]
+        if torch._C._cuda_getDevice() == kv.index:  # (torch.cuda.device takes 1.3 us, this 0.1)
+            return fn(*args, **kw)
+        with torch.cuda.device(kv.index):
+            return fn(*args, **kw)
+    return call
 
 
+@_on_its_device
 def paged_append(kv: PagedKV, k: torch.Tensor, v: torch.Tensor, seqs: Seqs, kv_len: torch.Tensor,
                  pos: Optional[torch.Tensor] = None, rope_theta: float = 10000.0,
                  q: Optional[torch.Tensor] = None, n_heads: int = 0) -> Optional[torch.Tensor]:
@@ -451,13 +455,15 @@ def paged_append(kv: PagedKV, k: torch.Tensor, v: torch.Tensor, seqs: Seqs, kv_l
         out = q.new_empty((T, qos))
     if T == 0:
         return out
-    _on(kv.index, lib().zsa_paged_append, kv._ref, k.data_ptr(), ks, v.data_ptr(), vs,
+    _check(lib().zsa_paged_append(
+        torch._C._cuda_getCurrentRawStream(kv.index), kv._ref, k.data_ptr(), ks, v.data_ptr(), vs,
         None if q is None else q.data_ptr(), qs, n_heads, None if q is None else out.data_ptr(), qos,
         None if pos is None else pos.data_ptr(), rope_theta, seqs.batch, seqs.host_ptr(), seqs.dev.data_ptr(),
-        kv_len.data_ptr())
+        kv_len.data_ptr()))
     return out
 
 
+@_on_its_device
 def prefix_attention(q: torch.Tensor, kv: PagedKV, n_heads: int, seqs: Seqs, kv_len: torch.Tensor,
                      prefix_pages: Optional[torch.Tensor], prefix_len: int,
                      max_kv_len: Optional[int] = None, causal: bool = True, want_lse: bool = False,
@@ -475,7 +481,9 @@ def prefix_attention(q: torch.Tensor, kv: PagedKV, n_heads: int, seqs: Seqs, kv_
             raise ValueError("prefix_pages must be contiguous int32 ids, on the cache's device, of pages that hold "
                              "prefix_len rows")
     if max_kv_len is None:
-        max_kv_len = kv._struct.max_pages * size
+        max_kv_len = min(kv._struct.max_pages * size, 1 << 30)
+    if prefix_len > 1 << 30 or max_kv_len > 1 << 30:
+        raise ValueError("a prefix or sequence of more than 2^30 rows")
     if scale is None:
         scale = hd ** -0.5
     out = q.new_empty((T, width))
@@ -483,10 +491,11 @@ def prefix_attention(q: torch.Tensor, kv: PagedKV, n_heads: int, seqs: Seqs, kv_
     cu, l = seqs.host_ptr(), lib()
     wsz = l.zsa_paged_attention_workspace_size(kv._ref, n_heads, kv.batch, cu, max_kv_len, prefix_len)
     ws = q.new_empty(wsz, dtype=torch.uint8) if wsz else None
-    _on(kv.index, l.zsa_prefix_attention, kv._ref, q.data_ptr(), qs, n_heads, causal, scale, kv.batch, cu,
+    _check(l.zsa_prefix_attention(
+        torch._C._cuda_getCurrentRawStream(kv.index), kv._ref, q.data_ptr(), qs, n_heads, causal, scale, kv.batch, cu,
         seqs.dev.data_ptr(), kv_len.data_ptr(), max_kv_len,
         None if prefix_pages is None else prefix_pages.data_ptr(), prefix_len, out.data_ptr(), width,
-        None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), wsz)
+        None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), wsz))
     return out, lse
 
 

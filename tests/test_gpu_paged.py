@@ -448,6 +448,30 @@ def test_captured_calls_with_other_lengths():
     b.compare(want[2], want[3], *b.oracle(True))
 
 
+def test_arguments_by_name():
+    b = Batch("bf16", 4, 2, 64, 16, [1, 2], [30, 20], 20, seed=1)
+    want = b.run(True)
+    got = zsa.prefix_attention(q=b.q, kv=b.kvc, n_heads=4, seqs=zsa.Seqs.wrap(b.cu, b.seqs.dev), kv_len=b.len_dev,
+                               prefix_pages=b.head_dev, prefix_len=20, want_lse=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    k = torch.randn((3, 128), device=dev()).to(torch.bfloat16)
+    assert zsa.paged_append(kv=b.kvc, k=k, v=k, seqs=b.seqs, kv_len=b.len_dev) is None
+    out, lse = zsa.paged_attention(q=b.q, kv=b.kvc, n_heads=4, seqs=b.seqs, kv_len=b.len_dev)
+    assert lse is None and out.shape == b.q.shape
+
+
+def test_lengths_on_the_device_that_are_out_of_range():
+    # negative: no rows; beyond the bound: the rows up to it
+    b = Batch("bf16", 4, 2, 64, 16, [1, 2, 40], [30, 20, 60], 20, seed=1)
+    for lens in ([-5, 1 << 30, 2 ** 31 - 1], [-2 ** 31, 45, 64]):
+        b.len_dev.copy_(torch.tensor(lens, dtype=torch.int32))
+        b.lens = lens
+        out, lse = b.run(False, max_kv_len=20)
+        ref, rlse, size, mag = b.oracle(False, max_kv_len=20)
+        b.lens = [20] * 3
+        b.compare(out, lse, ref, rlse, size, mag)
+
+
 def test_nothing_to_do():
     b = Batch("bf16", 4, 2, 64, 16, [0, 0], [30, 0], seed=1)
     out, lse = b.run(True)
@@ -492,5 +516,9 @@ def test_python_refusals():
         zsa.PagedKV(b.pool, b.table_dev, 3)
     with pytest.raises(ValueError):
         zsa.PagedKV(b.pool.transpose(0, 1), b.table_dev, 2)
+    with pytest.raises(ValueError):
+        zsa.paged_attention(b.q, b.kvc, 4, b.seqs, b.len_dev, max_kv_len=(1 << 32) + 20)
+    with pytest.raises(ValueError):
+        zsa.prefix_attention(b.q, b.kvc, 4, b.seqs, b.len_dev, b.head_dev, (1 << 32) + 20)
     with pytest.raises(ValueError):
         zsa.Seqs.wrap([0, 1, 3], b.seqs.dev.long())
