@@ -149,6 +149,10 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   return p;
 }
 
+size_t workspace_of(const Plan& p, const zsa_paged_kv& kv, int T, int H) {
+  return p.join() ? parts_bytes(p.parts(), static_cast<int64_t>(T) * H, kv.head_dim) : 0;
+}
+
 int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_heads,
               int32_t causal, float scale, int32_t batch, const int32_t* cu_host, const int32_t* cu_dev,
               const int32_t* kv_len, int32_t max_kv_len, const int32_t* prefix_pages, int32_t prefix_len,
@@ -176,13 +180,11 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
     return set_error(ZSA_EUNSUPPORTED, "max_kv_len %d, prefix_len %d beyond 2^30", max_kv_len, prefix_len);
   if (static_cast<int64_t>(T) * n_heads >= (int64_t{1} << 30))
     return set_error(ZSA_EUNSUPPORTED, "%d rows of %d heads: 2^30 or more", T, n_heads);
-  const size_t need = zsa_paged_attention_workspace_size(kv, n_heads, batch, cu_host, max_kv_len, prefix_len);
-  if (need > 0) {
-    CHECK(check_ptr16(ws, "ws"));
-    if (ws_bytes < need) return set_error(ZSA_EWORKSPACE, "workspace %zu bytes < %zu", ws_bytes, need);
-  }
   if (T == 0) return ZSA_OK;
   const Plan p = plan_of(*kv, n_heads, batch, cu_host, max_kv_len, prefix_len);
+  const size_t need = workspace_of(p, *kv, T, n_heads);
+  if (ws_bytes < need) return set_error(ZSA_EWORKSPACE, "workspace %zu bytes < %zu", ws_bytes, need);
+  if (need > 0) CHECK(check_ptr16(ws, "ws"));
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int64_t rows = static_cast<int64_t>(T) * n_heads;
   float2* ml = p.join() ? static_cast<float2*>(ws) : nullptr;
@@ -317,7 +319,7 @@ size_t zsa_paged_attention_workspace_size(const zsa_paged_kv* kv, int32_t n_head
   const int T = cu_host[batch];
   if (T <= 0) return 0;
   const Plan p = plan_of(*kv, n_heads, batch, cu_host, max_kv_len, prefix_len);
-  return !p.join() ? 0 : parts_bytes(p.parts(), static_cast<int64_t>(T) * n_heads, kv->head_dim);
+  return workspace_of(p, *kv, T, n_heads);
 }
 
 int zsa_paged_attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_heads,

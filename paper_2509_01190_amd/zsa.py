@@ -9,7 +9,6 @@ else.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -420,19 +419,6 @@ def _rows_stride(kv: PagedKV, rows: torch.Tensor, total: int, cols: int, what: s
     return stride if total > 1 else cols
 
 
-def _on_its_device(fn):
-    """The call with the cache's device current, whichever is."""
-    @functools.wraps(fn)
-    def call(*args, **kw):
-        kv = kw["kv"] if "kv" in kw else args[0] if isinstance(args[0], PagedKV) else args[1]
-        if torch._C._cuda_getDevice() == kv.index:  # (torch.cuda.device takes 1.3 us, this 0.1)
-            return fn(*args, **kw)
-        with torch.cuda.device(kv.index):
-            return fn(*args, **kw)
-    return call
-
-
-@_on_its_device
 def paged_append(kv: PagedKV, k: torch.Tensor, v: torch.Tensor, seqs: Seqs, kv_len: torch.Tensor,
                  pos: Optional[torch.Tensor] = None, rope_theta: float = 10000.0,
                  q: Optional[torch.Tensor] = None, n_heads: int = 0) -> Optional[torch.Tensor]:
@@ -441,6 +427,9 @@ def paged_append(kv: PagedKV, k: torch.Tensor, v: torch.Tensor, seqs: Seqs, kv_l
     sequence's rows with the new ones, which are the last. With ``pos`` [T]
     int32 the keys are rotated on the way, and so are the queries ``q``
     [T, n_heads * hd] if given, which are returned."""
+    if torch._C._cuda_getDevice() != kv.index:  # (torch.cuda.device where it is current takes 1.3 us, this 0.1)
+        with torch.cuda.device(kv.index):
+            return paged_append(kv, k, v, seqs, kv_len, pos, rope_theta, q, n_heads)
     _paged_rows(kv, seqs, kv_len)
     T = seqs.total
     kvd = kv.n_kv_heads * kv.head_dim
@@ -463,7 +452,6 @@ def paged_append(kv: PagedKV, k: torch.Tensor, v: torch.Tensor, seqs: Seqs, kv_l
     return out
 
 
-@_on_its_device
 def prefix_attention(q: torch.Tensor, kv: PagedKV, n_heads: int, seqs: Seqs, kv_len: torch.Tensor,
                      prefix_pages: Optional[torch.Tensor], prefix_len: int,
                      max_kv_len: Optional[int] = None, causal: bool = True, want_lse: bool = False,
@@ -471,6 +459,10 @@ def prefix_attention(q: torch.Tensor, kv: PagedKV, n_heads: int, seqs: Seqs, kv_
     """paged_attention for sequences that share their first ``prefix_len``
     rows, which lie in the pages ``prefix_pages`` (int32, on the device)
     and come before the rows that kv_len counts. Returns (out, lse or None)."""
+    if torch._C._cuda_getDevice() != kv.index:
+        with torch.cuda.device(kv.index):
+            return prefix_attention(q, kv, n_heads, seqs, kv_len, prefix_pages, prefix_len, max_kv_len, causal,
+                                    want_lse, scale)
     _paged_rows(kv, seqs, kv_len)
     hd, size, T = kv.head_dim, kv._struct.page_size, seqs.total
     width = n_heads * hd
@@ -488,15 +480,21 @@ def prefix_attention(q: torch.Tensor, kv: PagedKV, n_heads: int, seqs: Seqs, kv_
         scale = hd ** -0.5
     out = q.new_empty((T, width))
     lse = q.new_empty((n_heads, T), dtype=torch.float32) if want_lse else None
-    cu, l = seqs.host_ptr(), lib()
-    wsz = l.zsa_paged_attention_workspace_size(kv._ref, n_heads, kv.batch, cu, max_kv_len, prefix_len)
-    ws = q.new_empty(wsz, dtype=torch.uint8) if wsz else None
-    _check(l.zsa_prefix_attention(
-        torch._C._cuda_getCurrentRawStream(kv.index), kv._ref, q.data_ptr(), qs, n_heads, causal, scale, kv.batch, cu,
-        seqs.dev.data_ptr(), kv_len.data_ptr(), max_kv_len,
-        None if prefix_pages is None else prefix_pages.data_ptr(), prefix_len, out.data_ptr(), width,
-        None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), wsz))
-    return out, lse
+    cu, l, ws, wsz = seqs.host_ptr(), lib(), None, 0
+    ask = max_kv_len + prefix_len > 1024  # shorter calls hardly ever need a workspace: asked when one is refused without
+    while True:
+        if ask:
+            wsz = l.zsa_paged_attention_workspace_size(kv._ref, n_heads, kv.batch, cu, max_kv_len, prefix_len)
+            ws = q.new_empty(wsz, dtype=torch.uint8) if wsz else None
+        rc = l.zsa_prefix_attention(
+            torch._C._cuda_getCurrentRawStream(kv.index), kv._ref, q.data_ptr(), qs, n_heads, causal, scale, kv.batch,
+            cu, seqs.dev.data_ptr(), kv_len.data_ptr(), max_kv_len,
+            None if prefix_pages is None else prefix_pages.data_ptr(), prefix_len, out.data_ptr(), width,
+            None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), wsz)
+        if rc != EWORKSPACE or ask:
+            _check(rc)
+            return out, lse
+        ask = True
 
 
 def paged_attention(q: torch.Tensor, kv: PagedKV, n_heads: int, seqs: Seqs, kv_len: torch.Tensor,

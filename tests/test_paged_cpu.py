@@ -78,7 +78,8 @@ def test_appends_that_are_refused(kw, code):
     (dict(dev=None), zsa.EINVAL), (dict(offs=(0, 2, 1)), zsa.ESHAPE), (dict(most=-1), zsa.EINVAL),
     (dict(most=65), zsa.ESHAPE),                                                 # beyond the table
     (dict(prefix=-1), zsa.EINVAL), (dict(prefix=20), zsa.EINVAL),                # no prefix pages
-    (dict(prefix=40000, pages=PTR[7]), zsa.EINVAL),                              # parts, and no workspace
+    (dict(prefix=40000, pages=PTR[7]), zsa.EWORKSPACE),
+    (dict(prefix=40000, pages=PTR[7], wsb=1 << 40), zsa.EINVAL),                              # parts, and no workspace
     (dict(prefix=40000, pages=PTR[7], ws=PTR[8], wsb=64), zsa.EWORKSPACE),
     (dict(prefix=40000, pages=PTR[7], ws=ODD, wsb=1 << 30), zsa.EALIGN),
     (dict(prefix=(1 << 30) + 1, pages=PTR[7]), zsa.EUNSUPPORTED),
