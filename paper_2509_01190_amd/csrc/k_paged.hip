@@ -192,21 +192,21 @@ __device__ __forceinline__ scalar_ids scalar(const int32_t* p) {
 // one row, keys 4 (l / 16) + r and those + 16, which are its operand of the
 // second product; V is read in that same order of keys. P meets V as two bf16
 // numbers whose sum has 16 bits: the matrix cores have the time.
-template <int HD>
-struct FewShared {  // LDS of a group of four waves
-  static constexpr int NW = 4, HP = 17;  // merge row stride: [channel][row]
+template <int HD, int NW>
+struct FewShared {  // LDS of a group of NW waves
+  static constexpr int HP = 17;  // merge row stride: [channel][row]
   static constexpr int TILES = NW * 64 * HD * 2, MERGE = NW * HD * HP * 4;
   unsigned char tiles[MERGE > TILES ? MERGE : TILES];
   float m[NW][16], l[NW][16];
 };
 
-// the work of one of `blocks` groups of four waves, as its thread `tid`; all threads of the workgroup call it
-template <int HD, bool HEAD>
-__device__ __forceinline__ void few_rows(const PagedAttention& a, int block, bool there, int tid, FewShared<HD>& shared) {
-  constexpr int NW = FewShared<HD>::NW, KK = HD / 32, CT = HD / 16, CPR = HD / 8;
+// the work of group `block` of NW waves (if there is one), as its thread `tid`; all threads of the workgroup call it
+template <int HD, int NW, bool HEAD>
+__device__ __forceinline__ void few_rows(const PagedAttention& a, int block, bool there, int tid, FewShared<HD, NW>& shared) {
+  constexpr int KK = HD / 32, CT = HD / 16, CPR = HD / 8;
   constexpr int RB = HD * 2, HALF = 32 * RB;    // a tile of 32 rows of K, or V
   constexpr int RPL = 1024 / RB, NL = 16 / RPL;  // rows a load, loads per 16 rows
-  constexpr int HP = FewShared<HD>::HP;
+  constexpr int HP = FewShared<HD, NW>::HP;
   unsigned char* smem = shared.tiles;
   auto& sm = shared.m;
   auto& sl = shared.l;
@@ -471,13 +471,13 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
   }
 }
 
-template <int HD, bool HEAD>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2))) void paged_few_kernel(
+template <int HD, int NW, bool HEAD>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 64 && NW == 4 ? 3 : 2))) void paged_few_kernel(
     PagedJobs jobs) {
-  __shared__ __align__(1024) FewShared<HD> shared;
+  __shared__ __align__(1024) FewShared<HD, NW> shared;
   const int which = blockIdx.x >= jobs.first;
   const PagedAttention a = jobs.job[which];  // (a copy: what it holds stays in registers)
-  few_rows<HD, HEAD>(a, blockIdx.x - (which ? jobs.first : 0), true, threadIdx.x, shared);
+  few_rows<HD, NW, HEAD>(a, blockIdx.x - (which ? jobs.first : 0), true, threadIdx.x, shared);
 }
 
 // bf16, heads of 64 and 128, many packed rows: bound by the products. A
@@ -924,10 +924,10 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
 template <int HD, int QB, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_many_kernel(PagedJobs many,
                                                                                                       PagedJobs few) {
-  constexpr int GROUPS = NW / FewShared<HD>::NW;
+  constexpr int GROUPS = NW / 4;
   __shared__ __align__(1024) union {
     ManyShared<HD, QB, NW> many;
-    FewShared<HD> few[GROUPS];
+    FewShared<HD, 4> few[GROUPS];
   } shared;
   if (blockIdx.x < many.blocks) {
     const int which = blockIdx.x >= many.first;
@@ -938,7 +938,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const uint32_t block = (blockIdx.x - many.blocks) * GROUPS + group;
     const int which = block >= few.first;
     const PagedAttention a = few.job[which];
-    few_rows<HD, false>(a, block - (which ? few.first : 0), block < few.blocks, threadIdx.x & 255, shared.few[group]);
+    few_rows<HD, 4, false>(a, block - (which ? few.first : 0), block < few.blocks, threadIdx.x & 255, shared.few[group]);
   }
 }
 
@@ -947,26 +947,26 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // number of packed rows, W = 16 or 32 at a time (one row costs what W do). K is read from LDS 16 bytes a lane, as the first
 // operand has it; V one number a lane, W consecutive channels a row. The
 // exponentials are expf (the fp32 attention in k_attn.hip says why).
-template <typename T, int HD, int W>
+template <typename T, int HD, int W, int NW>
 struct F32Shared {
-  static constexpr int NW = 4, HP = W + 1;  // merge row stride: [channel][row]
+  static constexpr int HP = W + 1;  // merge row stride: [channel][row]
   static constexpr int TILES = NW * 64 * HD * sizeof(T), MERGE = NW * HD * HP * 4;
   unsigned char tiles[MERGE > TILES ? MERGE : TILES];
   float m[NW][W], l[NW][W];
 };
 
-template <typename T, int HD, int W, bool HEAD>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 1 : HD == 64 ? 2 : 3))) void paged_f32_kernel(
+template <typename T, int HD, int W, int NW, bool HEAD>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 1 : HD == 64 || NW == 8 ? 2 : 3))) void paged_f32_kernel(
     PagedJobs jobs) {
-  constexpr int NW = 4, E = sizeof(T);
+  constexpr int E = sizeof(T);
   constexpr int NG = 64 / W, NT = 32 / W, NR = W * W / 64;  // lane groups, key tiles of a step, registers of a tile
   constexpr int KK = HD / (4 * NG);          // channels go 4 a lane and group
   constexpr int CT = HD < W ? 1 : HD / W;    // W-channel blocks of O (half empty at HD 16, W 32)
   typedef std::conditional_t<W == 32, f32x16_t, f32x4_t> acc_t;
   constexpr int RB = HD * E, HALF = 32 * RB, CPR = RB / 16;
   constexpr int RPL = 1024 / RB < 16 ? 1024 / RB : 16, NL = 16 / RPL;  // rows a load, loads per 16 rows
-  constexpr int HP = F32Shared<T, HD, W>::HP;
-  __shared__ __align__(1024) F32Shared<T, HD, W> shared;
+  constexpr int HP = F32Shared<T, HD, W, NW>::HP;
+  __shared__ __align__(1024) F32Shared<T, HD, W, NW> shared;
   unsigned char* smem = shared.tiles;
   auto& sm = shared.m;
   auto& sl = shared.l;
@@ -1320,31 +1320,41 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restric
     lse[static_cast<int64_t>(h) * Trows + t] = L == 0.f ? -INFINITY : LOG2 ? (M + log2f(L)) * kLn2 : M + logf(L);
 }
 
+template <typename T, int HD, int W, bool HEAD>
+hipError_t f32_launch(hipStream_t s, const PagedJobs& jobs) {
+  if constexpr (W == 16 && HD * sizeof(T) <= 256)
+    if (jobs.job[0].waves == 8)
+      return launch(K_ATTENTION, paged_f32_kernel<T, HD, W, 8, HEAD>, dim3(jobs.blocks), dim3(512), 0, s, jobs);
+  return launch(K_ATTENTION, paged_f32_kernel<T, HD, W, 4, HEAD>, dim3(jobs.blocks), dim3(256), 0, s, jobs);
+}
+
 template <typename T, int W, bool HEAD>
-hipError_t f32_dispatch(hipStream_t s, const PagedJobs& jobs, dim3 g) {
-  const dim3 block(256);
+hipError_t f32_dispatch(hipStream_t s, const PagedJobs& jobs) {
   switch (jobs.job[0].hd) {
-    case 16: return launch(K_ATTENTION, paged_f32_kernel<T, 16, W, HEAD>, g, block, 0, s, jobs);
-    case 32: return launch(K_ATTENTION, paged_f32_kernel<T, 32, W, HEAD>, g, block, 0, s, jobs);
+    case 16: return f32_launch<T, 16, W, HEAD>(s, jobs);
+    case 32: return f32_launch<T, 32, W, HEAD>(s, jobs);
     default: break;
   }
   if constexpr (sizeof(T) == 4) {
-    if (jobs.job[0].hd == 64) return launch(K_ATTENTION, paged_f32_kernel<T, 64, W, HEAD>, g, block, 0, s, jobs);
-    if (jobs.job[0].hd == 128) return launch(K_ATTENTION, paged_f32_kernel<T, 128, W, HEAD>, g, block, 0, s, jobs);
+    if (jobs.job[0].hd == 64) return f32_launch<T, 64, W, HEAD>(s, jobs);
+    if (jobs.job[0].hd == 128) return f32_launch<T, 128, W, HEAD>(s, jobs);
   }
   return hipErrorInvalidValue;
 }
 
+template <int HD, bool HEAD>
+hipError_t few_launch(hipStream_t s, const PagedJobs& jobs) {
+  if (jobs.job[0].waves == 8)
+    return launch(K_ATTENTION, paged_few_kernel<HD, 8, HEAD>, dim3(jobs.blocks), dim3(512), 0, s, jobs);
+  return launch(K_ATTENTION, paged_few_kernel<HD, 4, HEAD>, dim3(jobs.blocks), dim3(256), 0, s, jobs);
+}
+
 template <bool HEAD>
 hipError_t few_dispatch(hipStream_t s, int dtype, const PagedJobs& jobs) {
-  const dim3 g(jobs.blocks);
   const PagedAttention& a = jobs.job[0];
-  if (paged_matrix(dtype, a.hd)) {
-    if (a.hd == 64) return launch(K_ATTENTION, paged_few_kernel<64, HEAD>, g, dim3(256), 0, s, jobs);
-    return launch(K_ATTENTION, paged_few_kernel<128, HEAD>, g, dim3(256), 0, s, jobs);
-  }
-  if (a.tile == 32) return dtype == 1 ? f32_dispatch<bf16_t, 32, HEAD>(s, jobs, g) : f32_dispatch<float, 32, HEAD>(s, jobs, g);
-  return dtype == 1 ? f32_dispatch<bf16_t, 16, HEAD>(s, jobs, g) : f32_dispatch<float, 16, HEAD>(s, jobs, g);
+  if (paged_matrix(dtype, a.hd)) return a.hd == 64 ? few_launch<64, HEAD>(s, jobs) : few_launch<128, HEAD>(s, jobs);
+  if (a.tile == 32) return dtype == 1 ? f32_dispatch<bf16_t, 32, HEAD>(s, jobs) : f32_dispatch<float, 32, HEAD>(s, jobs);
+  return dtype == 1 ? f32_dispatch<bf16_t, 16, HEAD>(s, jobs) : f32_dispatch<float, 16, HEAD>(s, jobs);
 }
 
 template <typename T>
@@ -1379,9 +1389,17 @@ hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a) {
 
 bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 64; }
 
+// Waves of a few-row workgroup: eight where the workgroups do not fill the CUs
+// and every wave has more than two steps of 32 keys otherwise.
+int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t workgroups) {
+  const bool can = matrix || (tile == 16 && hd * (dtype == 1 ? 2 : 4) <= 256);
+  return can && max_len > 256 && workgroups <= device_cu_count() ? 8 : 4;
+}
+
 // Splits of the keys. The few-row kernels: enough workgroups for four a CU, of
-// 512 keys at least, and one for 1024 in bf16 or where they fill half the CUs: a second split needs the parts
-// joined. One split / two, us: 4 sequences of up to 1000 rows, 12 heads of 64,
+// 512 keys at least, and one for 1024 in bf16 or where they fill half the CUs
+// : a second split needs the parts joined.
+// One split / two, us: 4 sequences of up to 1000 rows, 12 heads of 64,
 // 11.0 / 14.6; 1 of 1000, 32 heads of 128 on 8, 12.1 / 14.3; 4 of 2000 16.6 / 14.3;
 // fp32, 1 of 1000, 12 heads of 64, 19.8 / 15.2, 16 of up to 1024 21.0 / 21.6.
 // The many-row kernel, whose workgroups are long and few a CU: the number whose
@@ -1394,7 +1412,8 @@ int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups,
   const int64_t wgs = std::max<int64_t>(workgroups, 1), cus = device_cu_count();
   const int least = many ? 256 : 512;
   const int64_t blocks = std::max(1, (max_len + least - 1) / least);
-  int64_t want = max_len <= 1024 && (matrix || 2 * wgs >= cus) ? 1 : std::min(blocks, std::max<int64_t>(1, (4 * cus + wgs - 1) / wgs));
+  const int single = matrix || 2 * wgs >= cus ? 1024 : 512;  // keys that one split takes
+  int64_t want = max_len <= single ? 1 : std::min(blocks, std::max<int64_t>(1, (4 * cus + wgs - 1) / wgs));
   if (many) {
     const double slots = (hd == 64 ? 2.0 : 1.0) * std::max<int64_t>(cus, 1), key = (hd == 64 ? 2.9 : 1.8) / 64;
     const double part = static_cast<double>(wgs) * kPagedManyRows * hd * 8 / 4e6;

@@ -463,6 +463,7 @@ struct PagedAttention {
   int causal;
   float scale;
   int tile, tiles;            // packed rows of a workgroup; of the longest sequence, how many of those
+  int waves;                  // of a few-row workgroup: 4 or 8
   int few_rows;               // a few-row launch takes the sequences of up to so many packed rows, a many-row one the others
   int chunk, splits;          // keys a split takes, a multiple of 128; splits
   int parts;                  // the call's parts from this launch's first on
@@ -478,6 +479,7 @@ bool paged_matrix(int dtype, int hd);  // the bf16 matrix kernels take these hea
 // keys a split of up to max_len rows takes, and how many splits that makes; joined: rows have other parts anyway; other: us of
 // few-row work beside many-row workgroups
 int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, bool joined, double other, int* splits);
+int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t workgroups);  // of a few-row workgroup
 int64_t paged_blocks(const PagedAttention& a, bool many);  // workgroups
 // one launch of up to two of each kind, of one type and head dim
 hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention* few, int fews,

@@ -90,6 +90,7 @@ constexpr int kFewRows = 32;
 struct Part {
   bool many;
   int tile, tiles;    // packed rows of a workgroup; of the longest sequence, how many of those
+  int waves;          // of a few-row workgroup
   int chunk, splits;  // 0 splits: there are none
   bool head;          // the common prefix goes before the sequences' rows
 };
@@ -116,7 +117,7 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
     most[many] = std::max(most[many], rows);
   }
   double other = 0;  // us of the few-row work: its cached rows, half the longest each, at 5 TB/s
-  auto part = [&](bool many, int64_t max_rows, int max_len, bool common) {
+  auto part = [&](bool many, int64_t max_rows, int max_len, bool common, bool alone) {
     Part l{};
     l.many = many;
     l.tile = many ? zsa::kPagedManyRows : !matrix && max_rows > 16 ? 32 : zsa::kPagedFewRows;
@@ -126,7 +127,8 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
       const int64_t rows = (cu[b + 1] - cu[b]) * G;
       if (many == (matrix && rows > kFewRows)) workgroups += (rows + l.tile - 1) / l.tile;
     }
-    l.chunk = zsa::paged_chunk(many, matrix, hd, max_len, workgroups * kv.n_kv_heads, prefix > 0, other, &l.splits);
+    l.waves = alone && !many ? zsa::paged_waves(matrix, kv.dtype, hd, l.tile, max_len, workgroups * kv.n_kv_heads) : 4;
+    l.chunk = zsa::paged_chunk(many, matrix, hd, max_len, workgroups * kv.n_kv_heads, !alone, other, &l.splits);
     if (!many) other += workgroups * kv.n_kv_heads * hd * 2.0 * esize(kv.dtype) * max_len / 2 / 5e6;
     return l;
   };
@@ -135,16 +137,16 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   // join (8 sequences of up to 41 rows behind 501, 12 heads of 64: 15.7 -> 11.3 us).
   const int64_t row = 2 * static_cast<int64_t>(kv.n_kv_heads) * hd * esize(kv.dtype);
   if (prefix > 0 && most[1] == 0 && static_cast<int64_t>(batch) * prefix * row <= (32 << 20) && max_len < (1 << 29)) {
-    p.few = part(false, most[0], (prefix + 31) / 32 * 32 + max_len, false);
+    p.few = part(false, most[0], (prefix + 31) / 32 * 32 + max_len, false, true);
     p.few.head = true;
     return p;
   }
-  if (most[0] > 0) p.few = part(false, most[0], max_len, false);
-  if (most[1] > 0) p.many = part(true, most[1], max_len, false);
+  if (most[0] > 0) p.few = part(false, most[0], max_len, false, prefix == 0 && most[1] == 0);
+  if (most[1] > 0) p.many = part(true, most[1], max_len, false, prefix == 0);
   if (prefix > 0) {
     // (one launch takes one width of tiles)
-    p.prefix = part(matrix && T * G > kFewRows, T * G, prefix, true);
-    if (!matrix && p.few.splits > 0 && p.few.tile != p.prefix.tile) p.few = part(false, std::max<int64_t>(most[0], 17), max_len, false);
+    p.prefix = part(matrix && T * G > kFewRows, T * G, prefix, true, false);
+    if (!matrix && p.few.splits > 0 && p.few.tile != p.prefix.tile) p.few = part(false, std::max<int64_t>(most[0], 17), max_len, false, false);
   }
   return p;
 }
@@ -217,6 +219,7 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
     const bool prefix = l == &p.prefix;
     x.tile = l->tile;
     x.tiles = l->tiles;
+    x.waves = l->waves;
     x.chunk = l->chunk;
     x.splits = l->splits;
     x.few_rows = prefix ? (l->many ? 0 : INT32_MAX) : p.many.splits > 0 ? kFewRows : INT32_MAX;
@@ -240,7 +243,7 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
       x.ml = ml + (prefix ? 0 : p.prefix.splits) * rows;
       x.o = o + (prefix ? 0 : p.prefix.splits) * rows * kv->head_dim;
     }
-    threads += zsa::paged_blocks(x, l->many) * (l->many && kv->head_dim == 128 ? 512 : 256);
+    threads += zsa::paged_blocks(x, l->many) * (l->waves == 8 || (l->many && kv->head_dim == 128) ? 512 : 256);
   }
   if (threads >= (int64_t{1} << 32) - 512)  // (what a grid holds)
     return set_error(ZSA_EUNSUPPORTED, "%d sequences of up to %d rows of %d heads: more workgroups than a grid holds",
