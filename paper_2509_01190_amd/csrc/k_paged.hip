@@ -1396,12 +1396,17 @@ int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t w
   return can && max_len > 256 && workgroups <= device_cu_count() ? 8 : 4;
 }
 
-// Splits of the keys. The few-row kernels: enough workgroups for four a CU, of
-// 512 keys at least, and one for 1024 in bf16 or where they fill half the CUs
-// : a second split needs the parts joined.
+// Splits of the keys. The few-row kernels: one for up to 1024 keys in bf16 or
+// where they fill half the CUs, else for 512, as a second split needs the parts
+// joined; beyond, of 512 keys at least, enough workgroups for four a CU, and in a
+// bf16 call of one job for eight (ragged sequences even out) while that makes no
+// more than 10 parts.
 // One split / two, us: 4 sequences of up to 1000 rows, 12 heads of 64,
 // 11.0 / 14.6; 1 of 1000, 32 heads of 128 on 8, 12.1 / 14.3; 4 of 2000 16.6 / 14.3;
 // fp32, 1 of 1000, 12 heads of 64, 19.8 / 15.2, 16 of up to 1024 21.0 / 21.6.
+// Four / eight a CU: 64 of up to 4096, 32 heads of 128 on 8, 122.5 / 118.4; 7 of
+// 18000, 32 of 64, 212 / 207; 16 of up to 6000, 32 of 128 on 8 (16 parts), 57.7 / 63.3;
+// 4 of 65536 (64 parts) 179 / 184.
 // The many-row kernel, whose workgroups are long and few a CU: the number whose
 // rounds over the CUs take least, with the parts' bytes. A workgroup takes 8 us
 // and 1.8 us for 64 keys of 128, or, two a CU, 2.9 of 64; parts are written
@@ -1413,7 +1418,9 @@ int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups,
   const int least = many ? 256 : 512;
   const int64_t blocks = std::max(1, (max_len + least - 1) / least);
   const int single = matrix || 2 * wgs >= cus ? 1024 : 512;  // keys that one split takes
-  int64_t want = max_len <= single ? 1 : std::min(blocks, std::max<int64_t>(1, (4 * cus + wgs - 1) / wgs));
+  const int64_t four = (4 * cus + wgs - 1) / wgs, eight = (8 * cus + wgs - 1) / wgs;
+  const int64_t even = matrix && !joined ? std::min<int64_t>(eight, 10) : 1;
+  int64_t want = max_len <= single ? 1 : std::min(blocks, std::max<int64_t>({1, four, even}));
   if (many) {
     const double slots = (hd == 64 ? 2.0 : 1.0) * std::max<int64_t>(cus, 1), key = (hd == 64 ? 2.9 : 1.8) / 64;
     const double part = static_cast<double>(wgs) * kPagedManyRows * hd * 8 / 4e6;
