@@ -82,8 +82,14 @@ size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
 }
 
 // Packed rows (new rows times query heads per key/value head) up to which a
-// sequence goes to the few-row kernel.
-constexpr int kFewRows = 32;
+// sequence goes to the few-row kernel: one or two workgroups of 16, where the
+// rows are read twice. us, two / the many-row kernel, 8 sequences, 32 packed
+// rows, 32 heads of 128 on 8: up to 508 rows 10.0 / 15.5, up to 3008 31.2 / 23.7;
+// 17 to 32 rows, 32 heads of 64, up to 2032 36.6 / 33.3. A common prefix, with
+// other parts to join in any case, of 4000 rows, 32 heads of 64: 40 rows 22.6 /
+// 26.3, 63 rows 30.5 / 33.4, of 6000, 32 of 128 on 8, 48 rows 17.0 / 16.5.
+int few_rows(int max_len) { return max_len <= 1024 ? 32 : 16; }
+int few_prefix_rows(int hd) { return hd == 64 ? 64 : 32; }
 
 // The rows of one kind: the common prefix's, or the own ones of the sequences
 // of few packed rows, or of many.
@@ -110,10 +116,11 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   const int hd = kv.head_dim;
   const int64_t G = H / kv.n_kv_heads, T = cu[batch];
   const bool matrix = zsa::paged_matrix(kv.dtype, hd);
+  const int limit = few_rows(max_len);
   int64_t most[2] = {0, 0};
   for (int b = 0; b < batch; ++b) {
     const int64_t rows = (cu[b + 1] - cu[b]) * G;
-    const bool many = matrix && rows > kFewRows;
+    const bool many = matrix && rows > limit;
     most[many] = std::max(most[many], rows);
   }
   double other = 0;  // us of the few-row work: its cached rows, half the longest each, at 5 TB/s
@@ -125,7 +132,7 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
     int64_t workgroups = common ? l.tiles : 0;
     for (int b = 0; b < batch && !common; ++b) {
       const int64_t rows = (cu[b + 1] - cu[b]) * G;
-      if (many == (matrix && rows > kFewRows)) workgroups += (rows + l.tile - 1) / l.tile;
+      if (many == (matrix && rows > limit)) workgroups += (rows + l.tile - 1) / l.tile;
     }
     l.waves = alone && !many ? zsa::paged_waves(matrix, kv.dtype, hd, l.tile, max_len, workgroups * kv.n_kv_heads) : 4;
     l.chunk = zsa::paged_chunk(many, matrix, hd, max_len, workgroups * kv.n_kv_heads, !alone, other, &l.splits);
@@ -145,7 +152,7 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   if (most[1] > 0) p.many = part(true, most[1], max_len, false, prefix == 0);
   if (prefix > 0) {
     // (one launch takes one width of tiles)
-    p.prefix = part(matrix && T * G > kFewRows, T * G, prefix, true, false);
+    p.prefix = part(matrix && T * G > few_prefix_rows(hd), T * G, prefix, true, false);
     if (!matrix && p.few.splits > 0 && p.few.tile != p.prefix.tile) p.few = part(false, std::max<int64_t>(most[0], 17), max_len, false, false);
   }
   return p;
@@ -222,7 +229,7 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
     x.waves = l->waves;
     x.chunk = l->chunk;
     x.splits = l->splits;
-    x.few_rows = prefix ? (l->many ? 0 : INT32_MAX) : p.many.splits > 0 ? kFewRows : INT32_MAX;
+    x.few_rows = prefix ? (l->many ? 0 : INT32_MAX) : p.many.splits > 0 ? few_rows(max_kv_len) : INT32_MAX;
     x.parts = prefix ? l->splits : p.own();
     x.direct = p.direct(*l);
     if (l->head) {
