@@ -176,6 +176,16 @@ __device__ __forceinline__ void empty_parts(const PagedAttention& a, int64_t at)
   for (int p = a.splits; p < a.parts; ++p) a.ml[at + static_cast<int64_t>(p) * a.T * a.H] = make_float2(-INFINITY, 0.f);
 }
 
+// lds_load16 of rows that no other workgroup reads, too many to stay in the
+// last-level cache: they do not displace what is there. One row of 64 sequences
+// of up to 4096, 32 heads of 128 on 8, 102.9 us (5.4 TB/s), with lds_load16
+// 117.9. Where other workgroups read them too it loses (63 rows over 4000 common
+// ones, 32 heads of 64, 36.2 / 31.1), and where the next call finds them in the
+// cache (52 MB of fp32 rows 20.5 / 19.3).
+__device__ __forceinline__ void lds_load16_once(uint32_t lds, uint32_t off, const u32x4& res) {
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"{m0}"(lds), "v"(off), "s"(res) : "memory");
+}
+
 // the page ids and lengths, read as scalars: loads that would wait in line
 // with a wave's tile loads otherwise
 typedef const __attribute__((address_space(4))) int32_t* scalar_ids;
@@ -269,13 +279,19 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
     const int page = most >= 0 ? (first ? head_table : table)[min(p, most)] : -1;
     return j < (first ? a.head_len : end) ? page : -1;
   };
+  const bool once = !HEAD && a.once && a.tiles == 1;  // this workgroup alone reads the rows
   const uint32_t kcol = g * RB, vcol = rowb / 2 + g * RB;
   auto load = [&](int j0, int pg0, int pg1, uint32_t lds, uint32_t col, const uint32_t (&off)[NL]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const u32x4 res = resource(j0 + 16 * h, h == 0 ? pg0 : pg1, col);
+      if (once) {
 #pragma unroll
-      for (int i = 0; i < NL; ++i) lds_load16(lds + (h * NL + i) * 1024, off[i], res);
+        for (int i = 0; i < NL; ++i) lds_load16_once(lds + (h * NL + i) * 1024, off[i], res);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) lds_load16(lds + (h * NL + i) * 1024, off[i], res);
+      }
     }
   };
 
@@ -1032,14 +1048,21 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
     const int page = most >= 0 ? (first ? head_table : table)[min(p, most)] : -1;
     return j < (first ? a.head_len : end) ? page : -1;
   };
+  const bool once = !HEAD && a.once && a.tiles == 1;  // this workgroup alone reads the rows
   const uint32_t kcol = g * RB, vcol = rowb / 2 + g * RB;
   auto load = [&](int j0, int pg0, int pg1, uint32_t lds, uint32_t col, const uint32_t (&off)[NL]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const u32x4 res = resource(j0 + 16 * h, h == 0 ? pg0 : pg1, col);
+      if (once) {
 #pragma unroll
-      for (int i = 0; i < NL; ++i)
-        if (RPL * CPR == 64 || lane < RPL * CPR) lds_load16(lds + (h * NL + i) * (RPL * RB), off[i], res);
+        for (int i = 0; i < NL; ++i)
+          if (RPL * CPR == 64 || lane < RPL * CPR) lds_load16_once(lds + (h * NL + i) * (RPL * RB), off[i], res);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NL; ++i)
+          if (RPL * CPR == 64 || lane < RPL * CPR) lds_load16(lds + (h * NL + i) * (RPL * RB), off[i], res);
+      }
     }
   };
 

@@ -215,6 +215,10 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
   a.out = out;
   a.out_stride = out_stride;
   a.lse = lse;
+  // The call's cached rows, half the longest each. From 64 MB on, a quarter of
+  // the last-level cache, a program with more than one layer finds none of them
+  // there again.
+  const double cached = (batch * 0.5 * max_kv_len + prefix_len) * 2 * kv->n_kv_heads * kv->head_dim * esize(kv->dtype);
   // the work of the few-row kernel and of the many-row one
   zsa::PagedAttention job[2][2];
   int jobs[2] = {0, 0};
@@ -227,6 +231,7 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
     x.tile = l->tile;
     x.tiles = l->tiles;
     x.waves = l->waves;
+    x.once = cached >= 64e6;
     x.chunk = l->chunk;
     x.splits = l->splits;
     x.few_rows = prefix ? (l->many ? 0 : INT32_MAX) : p.many.splits > 0 ? few_rows(max_kv_len) : INT32_MAX;
