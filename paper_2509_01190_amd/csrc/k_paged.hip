@@ -1430,39 +1430,49 @@ int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t w
   return can && max_len > 256 && workgroups <= device_cu_count() ? 8 : 4;
 }
 
-// Splits of the keys. The few-row kernels: one for up to 1024 keys in bf16 or
-// where they fill half the CUs, else for 512, as a second split needs the parts
-// joined; beyond, of 512 keys at least, enough workgroups for four a CU, and in a
-// bf16 call of one job for eight (ragged sequences even out) while that makes no
-// more than 10 parts.
-// One split / two, us: 4 sequences of up to 1000 rows, 12 heads of 64,
-// 11.0 / 14.6; 1 of 1000, 32 heads of 128 on 8, 12.1 / 14.3; 4 of 2000 16.6 / 14.3;
-// fp32, 1 of 1000, 12 heads of 64, 19.8 / 15.2, 16 of up to 1024 21.0 / 21.6.
-// Four / eight a CU: 64 of up to 4096, 32 heads of 128 on 8, 122.5 / 118.4; 7 of
-// 18000, 32 of 64, 212 / 207; 16 of up to 6000, 32 of 128 on 8 (16 parts), 57.7 / 63.3;
-// 4 of 65536 (64 parts) 179 / 184.
+// Splits of the keys; a second one needs the parts joined.
+//
+// The few-row kernels: one for up to 1024 keys in bf16 or where the workgroups
+// fill half the CUs, else for 512 (one split / two, us: 4 sequences of up to 1000
+// rows, 12 heads of 64, 11.0 / 14.6; 1 of 1000, 32 heads of 128 on 8, 12.1 / 14.3;
+// 4 of 2000 16.6 / 14.3; fp32, 1 of 1000, 12 heads of 64, 19.8 / 15.2, 16 of up to
+// 1024 21.0 / 21.6). Longer, of 512 keys at least:
+//  * few workgroups: one a CU, and not a few more than that, which would take
+//    twice as long as the rest (4 sequences of 65536, 32 heads of 128 on 8, in
+//    6, 8, 16, 31 splits 168, 156, 159, 164; 9 of up to 14000, 24 of 64 on 8, in 3, 4,
+//    8 splits 49.6, 63.2, 48.4; 16 of up to 10000, 8 of 128 on 1, in 10, 16, 24
+//    17.6, 17.6, 23.2; fp32, 20 of up to 3000, 24 of 64 on 8, in 1, 2, 4 42.3, 34.7, 42.5);
+//  * many: ragged sequences even out over a few splits each (64 of up to 4096, 32
+//    of 128 on 8, in 1, 2, 4, 8 111, 109, 103, 105; 32 of up to 6000 in 1, 4, 6
+//    89, 85, 92; 7 of 18000, 32 of 64, in 1, 4, 10 187, 191, 180), two beside other
+//    jobs, whose rows would have as many parts.
+//
 // The many-row kernel, whose workgroups are long and few a CU: the number whose
 // rounds over the CUs take least, with the parts' bytes. A workgroup takes 8 us
-// and 1.8 us for 64 keys of 128, or, two a CU, 2.9 of 64; parts are written
-// and read at 4 TB/s, and a join that nothing else needs is 4 us. Where the
-// launch has `other` us of few-row work that fills the CUs between, the sum
-// counts, not the rounds.
-int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, bool joined, double other, int* splits) {
-  const int64_t wgs = std::max<int64_t>(workgroups, 1), cus = device_cu_count();
+// and for 64 keys 1.8 us, in 64-wide heads 2.6 where two are on a CU; parts are
+// written and read at 2 TB/s, and a join that nothing else needs is 4 us. The
+// sequences of a batch are taken for 0.6 of the longest. Where the launch has
+// `other` us of few-row work that fills the CUs between, the sum counts, not
+// the rounds. (In 1, 2, 4 splits: 24 sequences of up to 2556 rows of which three
+// bring 509, 32 heads of 64, 62.3, 81.3, 93.5; 4 x 1024 over up to 8024, 32 of 128 on
+// 8, 364, 420, 481; 16 questions on 4097 common rows, 32 of 64, in 2, 3, 4 77.3, 66.7,
+// 69.4; 64 rows over 8192, 32 of 128 on 8, in 8, 11, 16 41.2, 36.2, 40.6.)
+int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, bool ragged, bool joined, double other, int* splits) {
+  const int64_t wgs = std::max<int64_t>(workgroups, 1), cus = std::max(device_cu_count(), 1);
   const int least = many ? 256 : 512;
   const int64_t blocks = std::max(1, (max_len + least - 1) / least);
-  const int single = matrix || 2 * wgs >= cus ? 1024 : 512;  // keys that one split takes
-  const int64_t four = (4 * cus + wgs - 1) / wgs, eight = (8 * cus + wgs - 1) / wgs;
-  const int64_t even = matrix && !joined ? std::min<int64_t>(eight, 10) : 1;
-  int64_t want = max_len <= single ? 1 : std::min(blocks, std::max<int64_t>({1, four, even}));
+  int64_t want = 1;
   if (many) {
-    const double slots = (hd == 64 ? 2.0 : 1.0) * std::max<int64_t>(cus, 1), key = (hd == 64 ? 2.9 : 1.8) / 64;
-    const double part = static_cast<double>(wgs) * kPagedManyRows * hd * 8 / 4e6;
+    const double part = static_cast<double>(wgs) * kPagedManyRows * hd * 8 / 2e6;
+    const double len = ragged ? 0.6 * max_len : max_len;
     double best = 0;
     for (int64_t n = 1; n <= std::min<int64_t>(blocks, 64); ++n) {
-      const int64_t per = (blocks + n - 1) / n;
+      const double chunk = static_cast<double>((blocks + n - 1) / n * least);
+      const int64_t active = wgs * std::min<int64_t>(n, static_cast<int64_t>(ceil(std::max(len, 1.0) / chunk)));
+      const int together = hd == 64 && active > cus ? 2 : 1;  // workgroups on a CU at a time
+      const double one = std::min(chunk, len) * (together == 2 ? 2.6 : 1.8) / 64 + 8;
+      const double rounds = static_cast<double>(active) / (together * cus);
       const bool parts = n > 1 || joined;
-      const double one = std::min<double>(per * least, max_len) * key + 8, rounds = wgs * n / slots;
       const double us = (other > 0 ? std::max(one, rounds * one + other) : ceil(rounds) * one) + (parts ? n * part : 0) +
                         (parts && !joined ? 4 : 0);
       if (n == 1 || us < best) {
@@ -1470,6 +1480,14 @@ int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups,
         want = n;
       }
     }
+  } else if (max_len > (matrix || 2 * wgs >= cus ? 1024 : 512)) {
+    if (wgs * 32 < cus * 25) {
+      want = (cus * 15 / 16 + wgs - 1) / wgs;
+      if (wgs * want > cus && wgs * (want - 1) * 32 >= cus * 25) --want;
+    } else {
+      want = joined || !matrix ? 2 : std::max(4, std::min(max_len / 1800, 10));
+    }
+    want = std::min(want, blocks);
   }
   const int per = static_cast<int>((blocks + want - 1) / want);
   *splits = static_cast<int>((blocks + per - 1) / per);

@@ -135,7 +135,8 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
       if (many == (matrix && rows > limit)) workgroups += (rows + l.tile - 1) / l.tile;
     }
     l.waves = alone && !many ? zsa::paged_waves(matrix, kv.dtype, hd, l.tile, max_len, workgroups * kv.n_kv_heads) : 4;
-    l.chunk = zsa::paged_chunk(many, matrix, hd, max_len, workgroups * kv.n_kv_heads, !alone, other, &l.splits);
+    l.chunk = zsa::paged_chunk(many, matrix, hd, max_len, workgroups * kv.n_kv_heads, !common && batch > 1, !alone,
+                               other, &l.splits);
     if (!many) other += workgroups * kv.n_kv_heads * hd * 2.0 * esize(kv.dtype) * max_len / 2 / 5e6;
     return l;
   };
