@@ -209,7 +209,11 @@ __device__ __forceinline__ scalar_ids scalar(const int32_t* p) {
 // page outside the pool. The transposed products leave a lane eight scores of
 // one row, keys 4 (l / 16) + r and those + 16, which are its operand of the
 // second product; V is read in that same order of keys. P meets V as two bf16
-// numbers whose sum has 16 bits: the matrix cores have the time.
+// numbers whose sum has 16 bits: the matrix cores have the time. 32 packed rows
+// at a time (the 32-wide products) took as long where the bytes bound it and
+// longer elsewhere (8 of 128 on 1, 16 of up to 10000 rows 20.4, 16 at a time 19.6).
+// One row of 64 sequences of up to 4096, 32 heads of 128 on 8: 98 us and 5 for
+// the join, 5.4 TB/s in all; of 4 of up to 65536 156, 6.1 TB/s.
 template <int HD, int NW>
 struct FewShared {  // LDS of a group of NW waves
   static constexpr int HP = 17;  // merge row stride: [channel][row]
@@ -520,6 +524,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 6
 //  * The resource ends with the sequence, so rows behind it read as zeros.
 //  * The packed rows put the G query heads that share a key/value head into
 //    one workgroup: its tiles are read once for all of them.
+//  * P is rounded to bf16 for the second product, as there: half a step of
+//    each probability, which the sums of many average out.
+// 4 x 1024 new rows over up to 8024, 32 heads of 128 on 8, 360 us, 1.06 PFLOP/s
+// (the few-row kernel 751); 4 x 1024 over 8192, 32 of 64, 303 us, 0.91.
 template <int HD, int QB, int NW>
 struct ManyShared {
   static constexpr int WQ = 32 * QB, BUF = 2 * 64 * HD * 2, NB = 3, OLD = HD + 8;
@@ -968,7 +976,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
 // fp32 storage, and bf16 at head dims 16 and 32: the few-row kernel with both
 // products on the fp32 matrix instructions, fp32 operands and sums, for any
-// number of packed rows, W = 16 or 32 at a time (one row costs what W do). K is read from LDS 16 bytes a lane, as the first
+// number of packed rows, W = 16 or 32 at a time (one row costs what W do; one of
+// 42 sequences of up to 867, 32 heads of 128 on 8, 81 us with 32, 63 with 16, and
+// 57.7, 4.2 TB/s, now; 16 of up to 1024, 12 of 64, 19.4, loads' and products'
+// latency in turn). K is read from LDS 16 bytes a lane, as the first
 // operand has it; V one number a lane, W consecutive channels a row. The
 // exponentials are expf (the fp32 attention in k_attn.hip says why).
 template <typename T, int HD, int W, int NW>
