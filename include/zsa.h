@@ -437,7 +437,8 @@ typedef struct zsa_paged_kv {
  *   pos     [T] int32 device: the rows' positions; NULL: stored as they are
  *   q       NULL, or the same rows' queries, n_heads heads: rotated to q_out
  *           (which may be q itself)
- * No two of a call's rows may go to one cached row. T = 0 launches nothing.
+ * No two of a call's rows may go to one cached row. T = 0 launches nothing;
+ * T stays below 2^24.
  */
 int zsa_paged_append(void* stream, const zsa_paged_kv* kv, const void* k, int64_t k_stride,
                      const void* v, int64_t v_stride, const void* q, int64_t q_stride,

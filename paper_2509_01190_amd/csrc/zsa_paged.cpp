@@ -142,7 +142,7 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   };
   // A short prefix is read once per sequence, in the same workgroups, where
   // that is at most 32 MB, from the L2s: no second job and mostly no parts to
-  // join (8 sequences of up to 41 rows behind 501, 12 heads of 64: 15.7 -> 11.3 us).
+  // join (8 sequences of up to 41 rows behind 501, 12 heads of 64: 15.0 -> 10.7 us).
   const int64_t row = 2 * static_cast<int64_t>(kv.n_kv_heads) * hd * esize(kv.dtype);
   if (prefix > 0 && most[1] == 0 && static_cast<int64_t>(batch) * prefix * row <= (32 << 20) && max_len < (1 << 29)) {
     p.few = part(false, most[0], (prefix + 31) / 32 * 32 + max_len, false, true);
@@ -258,7 +258,8 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
     }
     threads += zsa::paged_blocks(x, l->many) * (l->waves == 8 || (l->many && kv->head_dim == 128) ? 512 : 256);
   }
-  if (threads >= (int64_t{1} << 32) - 512)  // (what a grid holds)
+  // (what a grid holds; the join takes head_dim / 4 threads a row, eight times that at most)
+  if (std::max(threads, p.join() ? rows * kv->head_dim / 4 : 0) >= (int64_t{1} << 32) - 4096)
     return set_error(ZSA_EUNSUPPORTED, "%d sequences of up to %d rows of %d heads: more workgroups than a grid holds",
                      batch, max_new, n_heads);
   HIP_TRY(zsa::launch_paged_attention(s, kv->dtype, job[0], jobs[0], job[1], jobs[1]), "paged attention");
@@ -297,6 +298,7 @@ int zsa_paged_append(void* stream, const zsa_paged_kv* kv, const void* k, int64_
   }
   if (pos != nullptr && !(rope_theta > 0.f)) return set_error(ZSA_EINVAL, "rope_theta <= 0");
   if (T > 0 && kv_len == nullptr) return set_error(ZSA_EINVAL, "kv_len is NULL");
+  if (T >= (1 << 24)) return set_error(ZSA_EUNSUPPORTED, "%d rows in one call (2^24 or more)", T);
   if (T == 0) return ZSA_OK;
   zsa::PagedAppend a{};
   a.at = rows_of(*kv);

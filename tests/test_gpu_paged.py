@@ -217,6 +217,33 @@ def test_longest_sequence_is_bounded_on_the_host():
     b.check(True, max_kv_len=100)
 
 
+@pytest.mark.parametrize("dtype,H,kv,hd", [("bf16", 4, 2, 64), ("bf16", 8, 8, 128), ("f32", 4, 4, 64), ("f32", 4, 2, 128),
+                                           ("bf16", 4, 4, 32), ("bf16", 2, 1, 16)])
+@pytest.mark.parametrize("new,prefix", [([1, 1, 1], 0), ([1, 60, 1], 0), ([40, 90, 33], 0), ([1, 50, 1], 70)])
+def test_wide_tables(dtype, H, kv, hd, new, prefix):
+    # the bound is the table's width, far beyond the rows: many splits, most of
+    # them empty, and rows read past the caches
+    b = Batch(dtype, H, kv, hd, 32, new, [700, 260, 1], prefix, seed=hd + sum(new))
+    wide = torch.randint(0, b.pool.shape[0], (3, 9000), dtype=torch.int32, device=dev())
+    wide[:, :b.table.shape[1]] = b.table_dev
+    b.kvc, b.table = zsa.PagedKV(b.pool, wide, kv), wide.cpu().numpy()
+    b.check(True)
+    b.check(False, max_kv_len=100000)
+
+
+@pytest.mark.parametrize("dtype,H,kv,hd", [("bf16", 4, 1, 64), ("bf16", 2, 2, 128), ("f32", 2, 1, 32)])
+def test_many_sequences(dtype, H, kv, hd):
+    g = np.random.default_rng(hd)
+    lens = [int(n) for n in g.integers(0, 40, 300)]
+    new = [1 if b % 7 else int(g.integers(0, 30)) for b in range(300)]
+    Batch(dtype, H, kv, hd, 16, new, lens, 37, seed=hd).check(True)
+
+
+def test_lengths_beyond_the_bound_under_the_mask():
+    b = Batch("bf16", 4, 2, 64, 16, [3, 40], [90, 100], seed=4)
+    b.check(True, max_kv_len=70)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scores", [60.0, 3000.0])
 def test_large_scores(dtype, scores):

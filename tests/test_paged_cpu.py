@@ -64,6 +64,7 @@ def test_caches_that_are_refused(kw, code):
     (dict(q=PTR[2], qs=256, H=3, qo=PTR[3], qos=256, pos=PTR[4]), zsa.ESHAPE),    # 2 does not divide 3
     (dict(q=PTR[2], qs=256, H=0, qo=PTR[3], qos=256, pos=PTR[4]), zsa.EINVAL),
     (dict(q=PTR[2], qs=248, H=4, qo=PTR[3], qos=256, pos=PTR[4]), zsa.ESHAPE),
+    (dict(offs=(0, 1 << 24)), zsa.EUNSUPPORTED),
     (dict(q=PTR[2], qs=256, H=4, qo=ODD, qos=256, pos=PTR[4]), zsa.EALIGN),
 ])
 def test_appends_that_are_refused(kw, code):
