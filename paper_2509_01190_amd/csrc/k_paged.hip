@@ -1447,7 +1447,8 @@ int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t w
 // fill half the CUs, else for 512 (one split / two, us: 4 sequences of up to 1000
 // rows, 12 heads of 64, 11.0 / 14.6; 1 of 1000, 32 heads of 128 on 8, 12.1 / 14.3;
 // 4 of 2000 16.6 / 14.3; fp32, 1 of 1000, 12 heads of 64, 19.8 / 15.2, 16 of up to
-// 1024 21.0 / 21.6). Longer, of 512 keys at least:
+// 1024 21.0 / 21.6). Longer, of 512 keys at least, in fp32 of 256 where the CUs
+// hold that many (2 of up to 3089, 8 of 128 on 1, 15.4 / 21.0):
 //  * few workgroups: one a CU, and not a few more than that, which would take
 //    twice as long as the rest (4 sequences of 65536, 32 heads of 128 on 8, in
 //    6, 8, 16, 31 splits 168, 156, 159, 164; 9 of up to 14000, 24 of 64 on 8, in 3, 4,
@@ -1470,7 +1471,8 @@ int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t w
 // 69.4; 64 rows over 8192, 32 of 128 on 8, in 8, 11, 16 41.2, 36.2, 40.6.)
 int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, bool ragged, bool joined, double other, int* splits) {
   const int64_t wgs = std::max<int64_t>(workgroups, 1), cus = std::max(device_cu_count(), 1);
-  const int least = many ? 256 : 512;
+  const int64_t small = static_cast<int64_t>(max_len + 255) / 256 * wgs;
+  const int least = many || (!matrix && small <= cus) ? 256 : 512;
   const int64_t blocks = std::max(1, (max_len + least - 1) / least);
   int64_t want = 1;
   if (many) {

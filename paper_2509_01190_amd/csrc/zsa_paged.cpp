@@ -87,8 +87,11 @@ size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
 // rows, 32 heads of 128 on 8: up to 508 rows 10.0 / 15.5, up to 3008 31.2 / 23.7;
 // 17 to 32 rows, 32 heads of 64, up to 2032 36.6 / 33.3. A common prefix, with
 // other parts to join in any case, of 4000 rows, 32 heads of 64: 40 rows 22.6 /
-// 26.3, 63 rows 30.5 / 33.4, of 6000, 32 of 128 on 8, 48 rows 17.0 / 16.5.
-int few_rows(int max_len) { return max_len <= 1024 ? 32 : 16; }
+// 26.3, 63 rows 30.5 / 33.4, of 6000, 32 of 128 on 8, 48 rows 17.0 / 16.5. Where
+// all workgroups of 16 rows run at once over up to 1024 rows (`fits`), up to eight
+// of them: 34 sequences of up to 756 rows, 8 to 72 packed rows, 8 heads of 128 on
+// 1, 12.1 / 19.3; 3 of 60 to 100 rows over up to 600, 12 of 64, 8.4 / 19.0.
+int few_rows(int max_len, bool fits) { return max_len <= 1024 ? (fits ? 128 : 32) : 16; }
 int few_prefix_rows(int hd) { return hd == 64 ? 64 : 32; }
 
 // The rows of one kind: the common prefix's, or the own ones of the sequences
@@ -104,6 +107,7 @@ struct Part {
 // The parts of the prefix come first, the others' after them, in the same places.
 struct Plan {
   Part prefix, few, many;
+  int few_rows;  // packed rows up to which a sequence is one of the few
   int own() const { return std::max(few.splits, many.splits); }
   int parts() const { return prefix.splits + own(); }
   // rows are finished at once where they have no other part
@@ -116,7 +120,20 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   const int hd = kv.head_dim;
   const int64_t G = H / kv.n_kv_heads, T = cu[batch];
   const bool matrix = zsa::paged_matrix(kv.dtype, hd);
-  const int limit = few_rows(max_len);
+  int64_t longest = 0, sixteens = 0;  // packed rows of a sequence; blocks of 16 of all
+  for (int b = 0; b < batch; ++b) {
+    const int64_t rows = (cu[b + 1] - cu[b]) * G;
+    longest = std::max(longest, rows);
+    sixteens += (rows + 15) / 16;
+  }
+  const int64_t row = 2 * static_cast<int64_t>(kv.n_kv_heads) * hd * esize(kv.dtype);
+  const bool fits = sixteens * kv.n_kv_heads <= zsa::device_cu_count();
+  // A short prefix is read once per sequence, in the same workgroups, where
+  // that is at most 32 MB, from the L2s: no second job and mostly no parts to
+  // join (8 sequences of up to 41 rows behind 501, 12 heads of 64: 15.0 -> 10.7 us).
+  const int whole = (prefix + 31) / 32 * 32 + max_len;
+  const bool head = prefix > 0 && static_cast<int64_t>(batch) * prefix * row <= (32 << 20) && max_len < (1 << 29);
+  const int limit = p.few_rows = few_rows(head ? whole : max_len, fits && longest <= 128);
   int64_t most[2] = {0, 0};
   for (int b = 0; b < batch; ++b) {
     const int64_t rows = (cu[b + 1] - cu[b]) * G;
@@ -127,7 +144,8 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   auto part = [&](bool many, int64_t max_rows, int max_len, bool common, bool alone) {
     Part l{};
     l.many = many;
-    l.tile = many ? zsa::kPagedManyRows : !matrix && max_rows > 16 ? 32 : zsa::kPagedFewRows;
+    // (fp32: 32 rows a workgroup cost less than twice 16, and more than 16 on another CU)
+    l.tile = many ? zsa::kPagedManyRows : !matrix && max_rows > 16 && (common || !fits) ? 32 : zsa::kPagedFewRows;
     l.tiles = static_cast<int>((max_rows + l.tile - 1) / l.tile);
     int64_t workgroups = common ? l.tiles : 0;
     for (int b = 0; b < batch && !common; ++b) {
@@ -140,12 +158,8 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
     if (!many) other += workgroups * kv.n_kv_heads * hd * 2.0 * esize(kv.dtype) * max_len / 2 / 5e6;
     return l;
   };
-  // A short prefix is read once per sequence, in the same workgroups, where
-  // that is at most 32 MB, from the L2s: no second job and mostly no parts to
-  // join (8 sequences of up to 41 rows behind 501, 12 heads of 64: 15.0 -> 10.7 us).
-  const int64_t row = 2 * static_cast<int64_t>(kv.n_kv_heads) * hd * esize(kv.dtype);
-  if (prefix > 0 && most[1] == 0 && static_cast<int64_t>(batch) * prefix * row <= (32 << 20) && max_len < (1 << 29)) {
-    p.few = part(false, most[0], (prefix + 31) / 32 * 32 + max_len, false, true);
+  if (head && most[1] == 0) {
+    p.few = part(false, most[0], whole, false, true);
     p.few.head = true;
     return p;
   }
@@ -154,7 +168,10 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   if (prefix > 0) {
     // (one launch takes one width of tiles)
     p.prefix = part(matrix && T * G > few_prefix_rows(hd), T * G, prefix, true, false);
-    if (!matrix && p.few.splits > 0 && p.few.tile != p.prefix.tile) p.few = part(false, std::max<int64_t>(most[0], 17), max_len, false, false);
+    if (!matrix && p.few.splits > 0 && p.few.tile != p.prefix.tile) {
+      p.few.tile = p.prefix.tile;
+      p.few.tiles = static_cast<int>((most[0] + p.few.tile - 1) / p.few.tile);
+    }
   }
   return p;
 }
@@ -235,7 +252,7 @@ int attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_str
     x.once = cached >= 64e6;
     x.chunk = l->chunk;
     x.splits = l->splits;
-    x.few_rows = prefix ? (l->many ? 0 : INT32_MAX) : p.many.splits > 0 ? few_rows(max_kv_len) : INT32_MAX;
+    x.few_rows = prefix ? (l->many ? 0 : INT32_MAX) : p.many.splits > 0 ? p.few_rows : INT32_MAX;
     x.parts = prefix ? l->splits : p.own();
     x.direct = p.direct(*l);
     if (l->head) {

@@ -36,6 +36,7 @@ int set_error(int code, const char* fmt, ...) {
   va_end(ap);
   return code;
 }
+int device_cu_count() { return 256; }
 bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 64; }
 int paged_waves(bool, int, int, int, int, int64_t) { return 4; }
 int paged_chunk(bool many, bool, int, int max_len, int64_t workgroups, bool, bool, double, int* splits) {
