@@ -90,7 +90,9 @@ size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
 // 26.3, 63 rows 30.5 / 33.4, of 6000, 32 of 128 on 8, 48 rows 17.0 / 16.5. Where
 // all workgroups of 16 rows run at once over up to 1024 rows (`fits`), up to eight
 // of them: 34 sequences of up to 756 rows, 8 to 72 packed rows, 8 heads of 128 on
-// 1, 12.1 / 19.3; 3 of 60 to 100 rows over up to 600, 12 of 64, 8.4 / 19.0.
+// 1, 12.1 / 19.3; 3 of 60 to 100 rows over up to 600, 12 of 64, 8.4 / 19.0; with more
+// than run at once it loses (25 of 10 to 20 rows over up to 920, 32 of 128 on 8,
+// 35.1 / 24.7).
 int few_rows(int max_len, bool fits) { return max_len <= 1024 ? (fits ? 128 : 32) : 16; }
 int few_prefix_rows(int hd) { return hd == 64 ? 64 : 32; }
 
@@ -127,7 +129,9 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
     sixteens += (rows + 15) / 16;
   }
   const int64_t row = 2 * static_cast<int64_t>(kv.n_kv_heads) * hd * esize(kv.dtype);
-  const bool fits = sixteens * kv.n_kv_heads <= zsa::device_cu_count();
+  // (what LDS holds of the few-row kernels' workgroups, a CU)
+  const int resident = 512 / (hd * static_cast<int>(esize(kv.dtype)));
+  const bool fits = sixteens * kv.n_kv_heads <= static_cast<int64_t>(zsa::device_cu_count()) * std::min(resident, 4);
   // A short prefix is read once per sequence, in the same workgroups, where
   // that is at most 32 MB, from the L2s: no second job and mostly no parts to
   // join (8 sequences of up to 41 rows behind 501, 12 heads of 64: 15.0 -> 10.7 us).
