@@ -198,13 +198,13 @@ __device__ __forceinline__ scalar_ids scalar(const int32_t* p) {
 // XCD L % 8: with the splits fastest and 2, 4 or 8 of them a ragged batch's
 // last splits, mostly empty, were all on the same XCDs.
 
-// bf16, heads of 64 and 128, 16 packed rows at a time: bound by the
+// bf16, heads of 32, 64 and 128, 16 packed rows at a time: bound by the
 // cached rows' bytes. A workgroup takes 16 packed rows of one (sequence,
 // key/value head) and a split of its keys; its four waves take 32-key tiles in
 // turn, each through its own K and V buffer in LDS, without barriers: the next
 // tile's K is under way as soon as S^T = K Q^T has read the last one, its V
 // after O^T += V^T P^T has. A load instruction covers whole rows of a head (4
-// of 128, 8 of 64) of one page, through a buffer resource that ends with the
+// of 128, 8 of 64, 16 of 32) of one page, through a buffer resource that ends with the
 // sequence, so what lies behind its last row reads as zeros, and so does a
 // page outside the pool. The transposed products leave a lane eight scores of
 // one row, keys 4 (l / 16) + r and those + 16, which are its operand of the
@@ -251,8 +251,8 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
   const float scale_log2 = a.scale * kLog2e;
 
   // K row r of a tile keeps its 16-byte chunk c at c ^ ksw(r), V row r at c ^ vsw(r) (k_attn.hip)
-  auto ksw = [](int r) { return HD == 64 ? (r >> 1) & 7 : r & 15; };
-  auto vsw = [](int r) { return HD == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; };
+  auto ksw = [](int r) { return HD == 32 ? (r >> 2) & 3 : HD == 64 ? (r >> 1) & 7 : r & 15; };
+  auto vsw = [](int r) { return HD == 32 ? 0 : HD == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; };
   const uint32_t rowb = static_cast<uint32_t>(a.at.kvd) * 4u;
   uint32_t koff[NL], voff[NL];
 #pragma unroll
@@ -500,7 +500,7 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
 }
 
 template <int HD, int NW, bool HEAD>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 64 && NW == 4 ? 3 : 2))) void paged_few_kernel(
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD <= 64 && NW == 4 ? 3 : 2))) void paged_few_kernel(
     PagedJobs jobs) {
   __shared__ __align__(1024) FewShared<HD, NW> shared;
   const int which = blockIdx.x >= jobs.first;
@@ -508,7 +508,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 6
   few_rows<HD, NW, HEAD>(a, blockIdx.x - (which ? jobs.first : 0), true, threadIdx.x, shared);
 }
 
-// bf16, heads of 64 and 128, many packed rows: bound by the products. A
+// bf16, heads of 32, 64 and 128, many packed rows: bound by the products. A
 // workgroup takes 32 QB NW packed rows of one (sequence, key/value head) and a
 // split of its keys; all waves share the K and V tiles of 64 keys, three of
 // them in LDS, loaded two ahead straight from the pages. A wave owns 32 QB rows
@@ -517,7 +517,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 6
 // moves only when it must: the order of the work, the tile layout and the
 // reasons are those of attn_wide_kernel (k_attn.hip). What differs is where a
 // tile's rows come from and which keys a row sees.
-//  * A load instruction covers rows of one page (4 of 128, 8 of 64 columns);
+//  * A load instruction covers rows of one page (4 of 128, 8 of 64, 16 of 32 columns);
 //    its page id is in a register of all lanes that holds the next 64 ids of
 //    the table, read 64 at a time: a scalar load would make every wait for LDS
 //    a wait for all of it, a vector load one for the tiles under way.
@@ -567,8 +567,8 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
   const bool busy = wq0 < sp.rows && wlast > k0;  // a wave without rows or keys only loads tiles
 
   const uint32_t rowb = static_cast<uint32_t>(a.at.kvd) * 4u;
-  auto ksw = [](int r) { return HD == 64 ? (r >> 1) & 7 : r & 15; };
-  auto vsw = [](int r) { return HD == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; };
+  auto ksw = [](int r) { return HD == 32 ? (r >> 2) & 3 : HD == 64 ? (r >> 1) & 7 : r & 15; };
+  auto vsw = [](int r) { return HD == 32 ? 0 : HD == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; };
   const int lrow = wave * RPL + lane / CPR;  // tile row of the wave's first load; the later ones are 16 n rows on
   const uint32_t koff = (lane / CPR) * rowb + (((lane % CPR) ^ ksw(lrow)) << 4);
   const uint32_t voff = (lane / CPR) * rowb + (((lane % CPR) ^ vsw(lrow)) << 4);
@@ -974,7 +974,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
-// fp32 storage, and bf16 at head dims 16 and 32: the few-row kernel with both
+// fp32 storage, and bf16 at head dim 16: the few-row kernel with both
 // products on the fp32 matrix instructions, fp32 operands and sums, for any
 // number of packed rows, W = 16 or 32 at a time (one row costs what W do; one of
 // 42 sequences of up to 867, 32 heads of 128 on 8, 81 us with 32, 63 with 16, and
@@ -1299,7 +1299,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restric
                                                          int H, int Trows, T* __restrict__ out,
                                                          int64_t out_stride, float* __restrict__ lse, int per) {
   constexpr int LPR = HD / 4, U = 4;
-  constexpr bool LOG2 = sizeof(T) == 2 && HD >= 64;
+  constexpr bool LOG2 = sizeof(T) == 2 && HD >= 32;
   __shared__ float sv[256][4];
   __shared__ float2 sml[256 / LPR];
   const int group = threadIdx.x / LPR, lane = threadIdx.x % LPR, sub = group % per, c = 4 * lane;
@@ -1372,12 +1372,9 @@ hipError_t f32_launch(hipStream_t s, const PagedJobs& jobs) {
 
 template <typename T, int W, bool HEAD>
 hipError_t f32_dispatch(hipStream_t s, const PagedJobs& jobs) {
-  switch (jobs.job[0].hd) {
-    case 16: return f32_launch<T, 16, W, HEAD>(s, jobs);
-    case 32: return f32_launch<T, 32, W, HEAD>(s, jobs);
-    default: break;
-  }
+  if (jobs.job[0].hd == 16) return f32_launch<T, 16, W, HEAD>(s, jobs);
   if constexpr (sizeof(T) == 4) {
+    if (jobs.job[0].hd == 32) return f32_launch<T, 32, W, HEAD>(s, jobs);
     if (jobs.job[0].hd == 64) return f32_launch<T, 64, W, HEAD>(s, jobs);
     if (jobs.job[0].hd == 128) return f32_launch<T, 128, W, HEAD>(s, jobs);
   }
@@ -1394,7 +1391,10 @@ hipError_t few_launch(hipStream_t s, const PagedJobs& jobs) {
 template <bool HEAD>
 hipError_t few_dispatch(hipStream_t s, int dtype, const PagedJobs& jobs) {
   const PagedAttention& a = jobs.job[0];
-  if (paged_matrix(dtype, a.hd)) return a.hd == 64 ? few_launch<64, HEAD>(s, jobs) : few_launch<128, HEAD>(s, jobs);
+  if (paged_matrix(dtype, a.hd)) {
+    if (a.hd == 32) return few_launch<32, HEAD>(s, jobs);
+    return a.hd == 64 ? few_launch<64, HEAD>(s, jobs) : few_launch<128, HEAD>(s, jobs);
+  }
   if (a.tile == 32) return dtype == 1 ? f32_dispatch<bf16_t, 32, HEAD>(s, jobs) : f32_dispatch<float, 32, HEAD>(s, jobs);
   return dtype == 1 ? f32_dispatch<bf16_t, 16, HEAD>(s, jobs) : f32_dispatch<float, 16, HEAD>(s, jobs);
 }
@@ -1432,7 +1432,7 @@ hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a) {
   return launch(K_MISC, paged_append_kernel<float>, grid, block, 0, s, a, rows);
 }
 
-bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 64; }
+bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 32; }
 
 // Waves of a few-row workgroup: eight where the workgroups do not fill the CUs
 // and every wave has more than two steps of 32 keys otherwise.
@@ -1461,7 +1461,7 @@ int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t w
 //
 // The many-row kernel, whose workgroups are long and few a CU: the number whose
 // rounds over the CUs take least, with the parts' bytes. A workgroup takes 8 us
-// and for 64 keys 1.8 us, in 64-wide heads 2.6 where two are on a CU; parts are
+// and for 64 keys 1.8 us, in heads below 128 2.6 where two are on a CU; parts are
 // written and read at 2 TB/s, and a join that nothing else needs is 4 us. The
 // sequences of a batch are taken for 0.6 of the longest. Where the launch has
 // `other` us of few-row work that fills the CUs between, the sum counts, not
@@ -1482,7 +1482,7 @@ int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups,
     for (int64_t n = 1; n <= std::min<int64_t>(blocks, 64); ++n) {
       const double chunk = static_cast<double>((blocks + n - 1) / n * least);
       const int64_t active = wgs * std::min<int64_t>(n, static_cast<int64_t>(ceil(std::max(len, 1.0) / chunk)));
-      const int together = hd == 64 && active > cus ? 2 : 1;  // workgroups on a CU at a time
+      const int together = hd < 128 && active > cus ? 2 : 1;  // workgroups on a CU at a time
       const double one = std::min(chunk, len) * (together == 2 ? 2.6 : 1.8) / 64 + 8;
       const double rounds = static_cast<double>(active) / (together * cus);
       const bool parts = n > 1 || joined;
@@ -1526,6 +1526,8 @@ hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention
   }
   const int hd = (manys > 0 ? many : few)[0].hd;
   if (manys > 0) {
+    if (hd == 32)
+      return launch(K_ATTENTION, paged_many_kernel<32, 2, 4>, dim3(w[1].blocks + w[0].blocks), dim3(256), 0, s, w[1], w[0]);
     if (hd == 64)
       return launch(K_ATTENTION, paged_many_kernel<64, 2, 4>, dim3(w[1].blocks + w[0].blocks), dim3(256), 0, s, w[1], w[0]);
     return launch(K_ATTENTION, paged_many_kernel<128, 1, 8>, dim3(w[1].blocks + (w[0].blocks + 1) / 2), dim3(512), 0, s, w[1], w[0]);

@@ -94,7 +94,7 @@ size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
 // than run at once it loses (25 of 10 to 20 rows over up to 920, 32 of 128 on 8,
 // 35.1 / 24.7).
 int few_rows(int max_len, bool fits) { return max_len <= 1024 ? (fits ? 128 : 32) : 16; }
-int few_prefix_rows(int hd) { return hd == 64 ? 64 : 32; }
+int few_prefix_rows(int hd) { return hd < 128 ? 64 : 32; }
 
 // The rows of one kind: the common prefix's, or the own ones of the sequences
 // of few packed rows, or of many.
