@@ -135,8 +135,8 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   // A short prefix is read once per sequence, in the same workgroups, where
   // that is at most 32 MB, from the L2s: no second job and mostly no parts to
   // join (8 sequences of up to 41 rows behind 501, 12 heads of 64: 15.0 -> 10.7 us).
-  const int whole = (prefix + 31) / 32 * 32 + max_len;
-  const bool head = prefix > 0 && static_cast<int64_t>(batch) * prefix * row <= (32 << 20) && max_len < (1 << 29);
+  const bool head = prefix > 0 && static_cast<double>(batch) * prefix * row <= (32 << 20) && max_len < (1 << 29);
+  const int whole = head ? (prefix + 31) / 32 * 32 + max_len : 0;
   const int limit = p.few_rows = few_rows(head ? whole : max_len, fits && longest <= 128);
   int64_t most[2] = {0, 0};
   for (int b = 0; b < batch; ++b) {
@@ -353,8 +353,9 @@ int zsa_paged_append(void* stream, const zsa_paged_kv* kv, const void* k, int64_
 size_t zsa_paged_attention_workspace_size(const zsa_paged_kv* kv, int32_t n_heads, int32_t batch,
                                           const int32_t* cu_host, int32_t max_kv_len, int32_t prefix_len) {
   if (kv == nullptr || cu_host == nullptr || batch <= 0 || n_heads <= 0 || kv->n_kv_heads <= 0 ||
-      n_heads % kv->n_kv_heads != 0 || max_kv_len < 0 || prefix_len < 0)
-    return 0;
+      n_heads % kv->n_kv_heads != 0 || max_kv_len < 0 || prefix_len < 0 || max_kv_len > (1 << 30) ||
+      prefix_len > (1 << 30) || check_head_dim(kv->head_dim) != ZSA_OK || check_dtype(kv->dtype) != ZSA_OK)
+    return 0;  // (the call itself refuses these)
   const int T = cu_host[batch];
   if (T <= 0) return 0;
   const Plan p = plan_of(*kv, n_heads, batch, cu_host, max_kv_len, prefix_len);

@@ -109,6 +109,24 @@ def test_workspace_is_that_of_the_parts():
     assert size(ctypes.byref(c), 4, 2, zsa._hp32(cu(0, 0, 0)), 64, 40000) == 0
 
 
+@pytest.mark.parametrize("kw,most,prefix", [
+    (dict(head_dim=0), 4096, 40000), (dict(head_dim=-16), 4096, 0), (dict(head_dim=48), 4096, 40000),
+    (dict(dtype=7), 4096, 40000), (dict(), (1 << 31) - 1, 0), (dict(), 64, (1 << 31) - 1),
+])
+def test_calls_that_are_refused_need_no_workspace(kw, most, prefix):
+    c, h = cache(max_pages=1 << 27, table_stride=1 << 27, **kw), cu(0, 1, 3)
+    assert zsa.lib().zsa_paged_attention_workspace_size(ctypes.byref(c), 4, 2, zsa._hp32(h), most, prefix) == 0
+    assert attend(c, qs=4096, os=4096, most=most, pages=PTR[7], prefix=prefix) in (zsa.EINVAL, zsa.EUNSUPPORTED, zsa.ESHAPE)
+
+
+@pytest.mark.parametrize("most,prefix", [(1 << 30, 0), (64, 1 << 30), (1 << 30, 1 << 30)])
+def test_workspace_of_the_longest(most, prefix):
+    c = cache(max_pages=1 << 26, table_stride=1 << 26)
+    h = np.arange(5001, dtype=np.int32)
+    size = zsa.lib().zsa_paged_attention_workspace_size
+    assert 5000 * 4 * 66 * 4 < size(ctypes.byref(c), 4, 5000, zsa._hp32(h), most, prefix) < 1 << 36
+
+
 # ---------------------------------------------------------------------------- the oracle
 def test_oracle_against_plain_softmax():
     g = np.random.default_rng(0)
