@@ -1441,19 +1441,42 @@ int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t w
   return can && max_len > 256 && workgroups <= device_cu_count() ? 8 : 4;
 }
 
-// Splits of the keys; a second one needs the parts joined.
+// Keys that a few-row workgroup takes in one split (see paged_chunk).
+static int paged_one(bool matrix, int hd, int64_t wgs, int64_t cus, int beside) {
+  if (beside == 2 && matrix) return 512;
+  if (beside == 0) {
+    if (wgs * 5 >= cus * 7) return 2048;
+    if (wgs <= cus && wgs * 16 >= cus * 11) return 4096;
+    if (matrix && wgs <= cus) return hd == 128 && wgs * 4 < cus ? 1152 : 1536;
+  }
+  return matrix || 2 * wgs >= cus ? 1024 : 512;
+}
+
+// Splits of the keys; a second one needs the parts joined. `beside`: 1 with jobs
+// of other sequences, 2 with a common prefix's.
 //
-// The few-row kernels: one for up to 1024 keys in bf16 or where the workgroups
-// fill half the CUs, else for 512 (one split / two, us: 4 sequences of up to 1000
-// rows, 12 heads of 64, 11.0 / 14.6; 1 of 1000, 32 heads of 128 on 8, 12.1 / 14.3;
-// 4 of 2000 16.6 / 14.3; fp32, 1 of 1000, 12 heads of 64, 19.8 / 15.2, 16 of up to
-// 1024 21.0 / 21.6). Longer, of 512 keys at least, in fp32 of 256 where the CUs
-// hold that many (2 of up to 3089, 8 of 128 on 1, 15.4 / 21.0):
+// The few-row kernels: one for as many keys as a second would not pay its
+// joining, 4 us and more (paged_one; us in one / two or three):
+//  * 11/16 of the CUs or more, up to one each: 4096 keys (24 sequences of up to
+//    3000 rows, 32 heads of 128 on 8, 48.8 / 55.6, of 8000 114 / 109; fp32, 25 of
+//    4000, 111 / 107, 24 of 64 on 8 63.5 / 63.9);
+//  * from 1.4 a CU: 2048 (64 of up to 1500, 32 of 128 on 8, 57.6 / 64, of 5000 181 /
+//    185; fp32, 64 of 2000, 145 / 153);
+//  * a few more than one a CU, which take twice as long as the rest: 1024 (40 of
+//    up to 1500, 32 of 128 on 8, 46.5 / 43.3; fp32, 40 of 2000 117 / 107);
+//  * fewer: 1536 (3 of up to 1500, 24 of 64 on 8, 11.3 / 12.3; 14 of 2000, 32 of 128
+//    on 8, 26.5 / 24.2), in heads of 128 on less than a quarter of the CUs 1152 (6
+//    of 1100 12.1 / 13.0, of 1500 15.0 / 13.5), in fp32 1024 or, under half of the
+//    CUs, 512 (1 of 1000, 12 of 64, 19.8 / 15.2; 16 of up to 1024 21.0 / 21.6);
+//  * beside a common prefix, where parts are joined in any case: in bf16 512 (20
+//    of up to 900, 32 of 128, behind 900 46.2 / 43.7).
+// Longer, of 512 keys at least, in fp32 of 256 where the CUs hold that many (2
+// of up to 3089, 8 of 128 on 1, 15.4 / 21.0):
 //  * few workgroups: one a CU, and not a few more than that, which would take
 //    twice as long as the rest (4 sequences of 65536, 32 heads of 128 on 8, in
 //    6, 8, 16, 31 splits 168, 156, 159, 164; 9 of up to 14000, 24 of 64 on 8, in 3, 4,
 //    8 splits 49.6, 63.2, 48.4; 16 of up to 10000, 8 of 128 on 1, in 10, 16, 24
-//    17.6, 17.6, 23.2; fp32, 20 of up to 3000, 24 of 64 on 8, in 1, 2, 4 42.3, 34.7, 42.5);
+//    17.6, 17.6, 23.2);
 //  * many: ragged sequences even out over a few splits each (64 of up to 4096, 32
 //    of 128 on 8, in 1, 2, 4, 8 111, 109, 103, 105; 32 of up to 6000 in 1, 4, 6
 //    89, 85, 92; 7 of 18000, 32 of 64, in 1, 4, 10 187, 191, 180), two beside other
@@ -1469,7 +1492,8 @@ int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t w
 // bring 509, 32 heads of 64, 62.3, 81.3, 93.5; 4 x 1024 over up to 8024, 32 of 128 on
 // 8, 364, 420, 481; 16 questions on 4097 common rows, 32 of 64, in 2, 3, 4 77.3, 66.7,
 // 69.4; 64 rows over 8192, 32 of 128 on 8, in 8, 11, 16 41.2, 36.2, 40.6.)
-int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, bool ragged, bool joined, double other, int* splits) {
+int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, bool ragged, int beside, double other, int* splits) {
+  const bool joined = beside > 0;
   const int64_t wgs = std::max<int64_t>(workgroups, 1), cus = std::max(device_cu_count(), 1);
   const int64_t small = static_cast<int64_t>(max_len + 255) / 256 * wgs;
   const int least = many || (!matrix && small <= cus) ? 256 : 512;
@@ -1493,8 +1517,8 @@ int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups,
         want = n;
       }
     }
-  } else if (max_len > (matrix || 2 * wgs >= cus ? 1024 : 512)) {
-    if (wgs * 32 < cus * 25) {
+  } else if (max_len > paged_one(matrix, hd, wgs, cus, beside)) {
+    if (wgs * 16 < cus * 11) {
       want = (cus * 15 / 16 + wgs - 1) / wgs;
       if (wgs * want > cus && wgs * (want - 1) * 32 >= cus * 25) --want;
     } else {

@@ -87,14 +87,22 @@ size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
 // rows, 32 heads of 128 on 8: up to 508 rows 10.0 / 15.5, up to 3008 31.2 / 23.7;
 // 17 to 32 rows, 32 heads of 64, up to 2032 36.6 / 33.3. A common prefix, with
 // other parts to join in any case, of 4000 rows, 32 heads of 64: 40 rows 22.6 /
-// 26.3, 63 rows 30.5 / 33.4, of 6000, 32 of 128 on 8, 48 rows 17.0 / 16.5. Where
+// 26.3, 63 rows 30.5 / 33.4, of 6000, 32 of 128 on 8, 48 rows 17.0 / 16.5. More rows
+// of a prefix where what the workgroups of 16 read, mostly from the L2s, is at
+// most 192 MB, in smaller heads 64 MB, and they are at most two a CU (32 of 128
+// on 8: 240 rows on 3000 22.9 / 25.6, on 8000 47 / 31; 12 of 64: 240 on 800 15.3 /
+// 18.7; 24 of 64 on 8: 180 on 3000, 74 MB, 18.8 / 18.1). Where
 // all workgroups of 16 rows run at once over up to 1024 rows (`fits`), up to eight
 // of them: 34 sequences of up to 756 rows, 8 to 72 packed rows, 8 heads of 128 on
 // 1, 12.1 / 19.3; 3 of 60 to 100 rows over up to 600, 12 of 64, 8.4 / 19.0; with more
 // than run at once it loses (25 of 10 to 20 rows over up to 920, 32 of 128 on 8,
 // 35.1 / 24.7).
 int few_rows(int max_len, bool fits) { return max_len <= 1024 ? (fits ? 128 : 32) : 16; }
-int few_prefix_rows(int hd) { return hd < 128 ? 64 : 32; }
+bool few_prefix(int hd, int kv_heads, int64_t rows, int prefix) {
+  const int64_t workgroups = (rows + 15) / 16 * kv_heads;
+  return rows <= (hd < 128 ? 64 : 32) || (workgroups <= 2 * zsa::device_cu_count() &&
+                                          workgroups * hd * 4.0 * prefix <= (hd < 128 ? 64 : 192) * 1048576.0);
+}
 
 // The rows of one kind: the common prefix's, or the own ones of the sequences
 // of few packed rows, or of many.
@@ -133,23 +141,40 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   const int resident = 512 / (hd * static_cast<int>(esize(kv.dtype)));
   const bool fits = sixteens * kv.n_kv_heads <= static_cast<int64_t>(zsa::device_cu_count()) * std::min(resident, 4);
   // A short prefix is read once per sequence, in the same workgroups, where
-  // that is at most 32 MB, from the L2s: no second job and mostly no parts to
-  // join (8 sequences of up to 41 rows behind 501, 12 heads of 64: 15.0 -> 10.7 us).
-  const bool head = prefix > 0 && static_cast<double>(batch) * prefix * row <= (32 << 20) && max_len < (1 << 29);
+  // that is at most 32 MB, from the L2s, or with the own rows 160 and no parts are
+  // to join then (8 sequences of up to 41 rows behind 501, 12 heads of 64: 15.0 ->
+  // 10.7 us; 30 x 4 rows over up to 100 behind 700, 32 of 128 on 8, 98 MB, 22.1 ->
+  // 12.6, 60 over up to 1000 behind 500, 370 MB, 36.9 -> 44.6; fp32, 55 x 4 over 10
+  // behind 99, 49 MB, 40 -> 25.7).
+  const double again = static_cast<double>(batch) * prefix * row / (1 << 20);
+  const bool head = prefix > 0 && (again <= 32 || again * (1.0 + static_cast<double>(max_len) / prefix) <= 160) &&
+                    max_len < (1 << 29);
   const int whole = head ? (prefix + 31) / 32 * 32 + max_len : 0;
-  const int limit = p.few_rows = few_rows(head ? whole : max_len, fits && longest <= 128);
-  int64_t most[2] = {0, 0};
-  for (int b = 0; b < batch; ++b) {
-    const int64_t rows = (cu[b + 1] - cu[b]) * G;
-    const bool many = matrix && rows > limit;
-    most[many] = std::max(most[many], rows);
-  }
+  int limit;
+  int64_t most[2];
+  auto sort = [&](int len) {
+    limit = p.few_rows = few_rows(len, fits && longest <= 128);
+    most[0] = most[1] = 0;
+    for (int b = 0; b < batch; ++b) {
+      const int64_t rows = (cu[b + 1] - cu[b]) * G;
+      const bool many = matrix && rows > limit;
+      most[many] = std::max(most[many], rows);
+    }
+  };
   double other = 0;  // us of the few-row work: its cached rows, half the longest each, at 5 TB/s
+  const int max_own = max_len;
   auto part = [&](bool many, int64_t max_rows, int max_len, bool common, bool alone) {
     Part l{};
     l.many = many;
-    // (fp32: 32 rows a workgroup cost less than twice 16, and more than 16 on another CU)
-    l.tile = many ? zsa::kPagedManyRows : !matrix && max_rows > 16 && (common || !fits) ? 32 : zsa::kPagedFewRows;
+    // fp32: 32 rows a workgroup cost less than twice 16, and more than 16 on
+    // another CU. One launch takes one width: the sequences' own, and 32 where the
+    // prefix is nearly all the work and long (in 16s / 32s, us: 60 rows behind 4000,
+    // 32 heads of 128 on 8, own rows up to 500, 94 / 111; 55 behind 300 24.7 / 30.4;
+    // 120 behind 12000, 16 heads of 64 on 2, 99 / 77).
+    const double pairs = static_cast<double>(T) * G * prefix;
+    const bool wide = common ? p.few.tile == 32 || (pairs * kv.n_kv_heads * hd >= 7e8 && pairs >= 64.0 * batch * max_own)
+                             : !fits;
+    l.tile = many ? zsa::kPagedManyRows : !matrix && max_rows > 16 && wide ? 32 : zsa::kPagedFewRows;
     l.tiles = static_cast<int>((max_rows + l.tile - 1) / l.tile);
     int64_t workgroups = common ? l.tiles : 0;
     for (int b = 0; b < batch && !common; ++b) {
@@ -157,21 +182,27 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
       if (many == (matrix && rows > limit)) workgroups += (rows + l.tile - 1) / l.tile;
     }
     l.waves = alone && !many ? zsa::paged_waves(matrix, kv.dtype, hd, l.tile, max_len, workgroups * kv.n_kv_heads) : 4;
-    l.chunk = zsa::paged_chunk(many, matrix, hd, max_len, workgroups * kv.n_kv_heads, !common && batch > 1, !alone,
-                               other, &l.splits);
+    l.chunk = zsa::paged_chunk(many, matrix, hd, max_len, workgroups * kv.n_kv_heads, !common && batch > 1,
+                               alone ? 0 : prefix > 0 ? 2 : 1, other, &l.splits);
     if (!many) other += workgroups * kv.n_kv_heads * hd * 2.0 * esize(kv.dtype) * max_len / 2 / 5e6;
     return l;
   };
-  if (head && most[1] == 0) {
-    p.few = part(false, most[0], whole, false, true);
-    p.few.head = true;
-    return p;
+  if (head) {
+    sort(whole);
+    if (most[1] == 0) {
+      p.few = part(false, most[0], whole, false, true);
+      p.few.head = true;
+      if (again <= 32 || p.few.splits == 1) return p;
+      p.few = Part{};
+      other = 0;
+    }
   }
+  sort(max_len);
   if (most[0] > 0) p.few = part(false, most[0], max_len, false, prefix == 0 && most[1] == 0);
   if (most[1] > 0) p.many = part(true, most[1], max_len, false, prefix == 0);
   if (prefix > 0) {
     // (one launch takes one width of tiles)
-    p.prefix = part(matrix && T * G > few_prefix_rows(hd), T * G, prefix, true, false);
+    p.prefix = part(matrix && !few_prefix(hd, kv.n_kv_heads, T * G, prefix), T * G, prefix, true, false);
     if (!matrix && p.few.splits > 0 && p.few.tile != p.prefix.tile) {
       p.few.tile = p.prefix.tile;
       p.few.tiles = static_cast<int>((most[0] + p.few.tile - 1) / p.few.tile);
