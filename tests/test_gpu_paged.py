@@ -160,6 +160,36 @@ def test_long_prefix_of_many_sequences(dtype, H, kv, hd, prefix, batch, n):
     Batch(dtype, H, kv, hd, 16, new, lens, prefix, seed=prefix + n).check(True)
 
 
+@pytest.mark.parametrize("dtype,H,kv,hd,prefix,batch,n", [
+    ("bf16", 16, 16, 128, 1500, 17, 1),
+    ("bf16", 32, 16, 128, 1500, 20, 1),   # 40 packed rows a head: three workgroups of the few-row kernel
+    ("bf16", 32, 16, 128, 1500, 20, 9),   # up to 360: the many-row kernel's
+    ("bf16", 16, 16, 64, 1500, 40, 3),    # up to 120 rows, in 16s
+    ("f32", 16, 16, 64, 1500, 24, 1),     # in 16s as the sequences' own rows
+    ("f32", 32, 16, 64, 1500, 24, 20),    # in 32s as those
+    ("f32", 16, 2, 64, 6000, 60, 2),      # in 32s for the prefix's length
+])
+def test_longer_prefix_of_many_sequences(dtype, H, kv, hd, prefix, batch, n):
+    # more than 160 MB if every sequence read it
+    new = [n if b % 3 else 1 for b in range(batch)]
+    lens = [m + (11 * b) % 70 for b, m in enumerate(new)]
+    lens[4] = 0
+    b = Batch(dtype, H, kv, hd, 64, new, lens, prefix, seed=prefix + n)
+    assert batch * prefix * 2 * kv * hd * (2 if dtype == "bf16" else 4) > 160 << 20
+    b.check(True)
+
+
+@pytest.mark.parametrize("dtype,H,kv,hd,batch,most", [
+    ("bf16", 8, 8, 64, 24, 2900), ("bf16", 16, 8, 128, 23, 2050), ("bf16", 8, 8, 32, 50, 1700), ("bf16", 4, 4, 64, 3, 1530),
+    ("f32", 8, 8, 64, 24, 2100), ("f32", 8, 8, 128, 50, 1100), ("bf16", 8, 8, 16, 24, 1300),
+])
+@pytest.mark.parametrize("prefix", [0, 37])
+def test_long_rows_in_one_split(dtype, H, kv, hd, batch, most, prefix):
+    lens = [most - (61 * b) % 1000 if b % 2 else 1 + 13 * b for b in range(batch)]
+    lens[0], lens[1] = most, 0
+    Batch(dtype, H, kv, hd, 64, [1] * batch, lens, prefix, seed=most).check(True, max_kv_len=most)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prefix_equals_the_same_rows_repeated(dtype):
     # the prefix cached once, against every sequence holding it as its own rows
