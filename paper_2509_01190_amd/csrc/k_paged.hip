@@ -1452,7 +1452,8 @@ static int paged_one(bool matrix, int hd, int64_t wgs, int64_t cus, int beside) 
   return matrix || 2 * wgs >= cus ? 1024 : 512;
 }
 
-// Splits of the keys; a second one needs the parts joined. `beside`: 1 with jobs
+// Splits of the keys; a second one needs the parts joined. `rows`: the packed
+// ones of all key/value heads. `beside`: 1 with jobs
 // of other sequences, 2 with a common prefix's.
 //
 // The few-row kernels: one for as many keys as a second would not pay its
@@ -1484,15 +1485,19 @@ static int paged_one(bool matrix, int hd, int64_t wgs, int64_t cus, int beside) 
 //
 // The many-row kernel, whose workgroups are long and few a CU: the number whose
 // rounds over the CUs take least, with the parts' bytes. A workgroup takes 8 us
-// and for 64 keys 1.8 us, in heads below 128 2.6 where two are on a CU; parts are
-// written and read at 2 TB/s, and a join that nothing else needs is 4 us. The
-// sequences of a batch are taken for 0.6 of the longest. Where the launch has
-// `other` us of few-row work that fills the CUs between, the sum counts, not
-// the rounds. (In 1, 2, 4 splits: 24 sequences of up to 2556 rows of which three
-// bring 509, 32 heads of 64, 62.3, 81.3, 93.5; 4 x 1024 over up to 8024, 32 of 128 on
-// 8, 364, 420, 481; 16 questions on 4097 common rows, 32 of 64, in 2, 3, 4 77.3, 66.7,
-// 69.4; 64 rows over 8192, 32 of 128 on 8, in 8, 11, 16 41.2, 36.2, 40.6.)
-int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, bool ragged, int beside, double other, int* splits) {
+// and for 64 keys 1.1 us where few of its rows are there, 1.8 where all are, in
+// heads below 128 1.4 to 2.6 where two are on a CU; parts are written and read at
+// 2 TB/s, and a join that nothing else needs is 4 us. The sequences of a batch are
+// taken as spread evenly from half of the longest on. Where the launch has `other`
+// us of few-row work that fills the CUs between, the sum counts, not the rounds.
+// (In 1, 2, 4 splits: 24 sequences of up to 2556 rows of which three bring 509, 32
+// heads of 64, 62.3, 81.3, 93.5; 4 x 1024 over up to 8024, 32 of 128 on 8, 364, 420,
+// 481; 16 questions on 4097 common rows, 32 of 64, in 2, 3, 4 77.3, 66.7, 69.4; 64 rows
+// over 8192, 32 of 128 on 8, in 8, 11, 16 41.2, 36.2, 40.6; 12 x 20 over up to 3020, 24
+// of 64 on 8, in 1, 2, 4, 6 64, 40, 27, 24. Over 80 such calls of 1 to 40 sequences it
+// is 3% from the best number.)
+int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, int64_t rows, bool ragged, int beside, double other,
+                int* splits) {
   const bool joined = beside > 0;
   const int64_t wgs = std::max<int64_t>(workgroups, 1), cus = std::max(device_cu_count(), 1);
   const int64_t small = static_cast<int64_t>(max_len + 255) / 256 * wgs;
@@ -1500,16 +1505,19 @@ int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups,
   const int64_t blocks = std::max(1, (max_len + least - 1) / least);
   int64_t want = 1;
   if (many) {
-    const double part = static_cast<double>(wgs) * kPagedManyRows * hd * 8 / 2e6;
-    const double len = ragged ? 0.6 * max_len : max_len;
+    const double part = static_cast<double>(rows) * hd * 8 / 2e6;
+    const double full = std::min(1.0, static_cast<double>(rows) / (wgs * kPagedManyRows));
     double best = 0;
     for (int64_t n = 1; n <= std::min<int64_t>(blocks, 64); ++n) {
       const double chunk = static_cast<double>((blocks + n - 1) / n * least);
-      const int64_t active = wgs * std::min<int64_t>(n, static_cast<int64_t>(ceil(std::max(len, 1.0) / chunk)));
-      const int together = hd < 128 && active > cus ? 2 : 1;  // workgroups on a CU at a time
-      const double one = std::min(chunk, len) * (together == 2 ? 2.6 : 1.8) / 64 + 8;
-      const double rounds = static_cast<double>(active) / (together * cus);
       const bool parts = n > 1 || joined;
+      double each = 0;  // parts of a sequence
+      for (int i = 0; i < 5; ++i) each += std::max(1.0, ceil((ragged ? 0.5 + 0.125 * i : 1) * max_len / chunk)) / 5;
+      const double active = wgs * each;
+      const int together = hd < 128 && active > cus ? 2 : 1;  // workgroups on a CU at a time
+      const double rounds = active / (together * cus);
+      const double len = ragged && (rounds > 1 || other > 0) ? 0.75 * max_len : max_len;
+      const double one = std::min(chunk, len) * (together == 2 ? 1.4 + 1.2 * full : 1.1 + 0.7 * full) / 64 + 8;
       const double us = (other > 0 ? std::max(one, rounds * one + other) : ceil(rounds) * one) + (parts ? n * part : 0) +
                         (parts && !joined ? 4 : 0);
       if (n == 1 || us < best) {

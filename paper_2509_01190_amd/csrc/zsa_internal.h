@@ -479,7 +479,8 @@ constexpr int kPagedManyRows = 256, kPagedFewRows = 16;  // packed rows of a wor
 bool paged_matrix(int dtype, int hd);  // the bf16 matrix kernels take these heads: one for few rows, one for many
 // keys a split of up to max_len rows takes, and how many splits that makes; joined: rows have other parts anyway; other: us of
 // few-row work beside many-row workgroups
-int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, bool ragged, int beside, double other, int* splits);
+int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, int64_t rows, bool ragged, int beside, double other,
+                int* splits);
 int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t workgroups);  // of a few-row workgroup
 int64_t paged_blocks(const PagedAttention& a, bool many);  // workgroups
 // one launch of up to two of each kind, of one type and head dim

@@ -92,12 +92,18 @@ size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
 // most 192 MB, in smaller heads 64 MB, and they are at most two a CU (32 of 128
 // on 8: 240 rows on 3000 22.9 / 25.6, on 8000 47 / 31; 12 of 64: 240 on 800 15.3 /
 // 18.7; 24 of 64 on 8: 180 on 3000, 74 MB, 18.8 / 18.1). Where
-// all workgroups of 16 rows run at once over up to 1024 rows (`fits`), up to eight
-// of them: 34 sequences of up to 756 rows, 8 to 72 packed rows, 8 heads of 128 on
-// 1, 12.1 / 19.3; 3 of 60 to 100 rows over up to 600, 12 of 64, 8.4 / 19.0; with more
-// than run at once it loses (25 of 10 to 20 rows over up to 920, 32 of 128 on 8,
-// 35.1 / 24.7).
-int few_rows(int max_len, bool fits) { return max_len <= 1024 ? (fits ? 128 : 32) : 16; }
+// all workgroups of 16 rows run at once (`fits`), up to eight of them over up to
+// 1536 rows: 34 sequences of up to 756 rows, 8 to 72 packed rows, 8 heads of 128
+// on 1, 12.1 / 19.3; 3 of 60 to 100 rows over up to 600, 12 of 64, 8.4 / 19.0; 12 of
+// 20 new rows over up to 1320, 24 of 64 on 8, 17.4 / 21.9; with more than run at
+// once it loses (25 of 10 to 20 rows over up to 920, 32 of 128 on 8, 35.1 / 24.7).
+// Two over up to 3072 in heads below 128 and at most one a CU (`one`): 12 of 8 new
+// rows, 24 of 64 on 8, 18.6 / 22.5; 40, with more, 68 / 59; 12, 32 of 128 on 8, 37.4
+// / 34.7.
+int few_rows(int max_len, int hd, bool fits, bool one) {
+  if (fits && max_len <= 1536) return 128;
+  return max_len <= (one && hd < 128 ? 3072 : 1024) ? 32 : 16;
+}
 bool few_prefix(int hd, int kv_heads, int64_t rows, int prefix) {
   const int64_t workgroups = (rows + 15) / 16 * kv_heads;
   return rows <= (hd < 128 ? 64 : 32) || (workgroups <= 2 * zsa::device_cu_count() &&
@@ -153,7 +159,7 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   int limit;
   int64_t most[2];
   auto sort = [&](int len) {
-    limit = p.few_rows = few_rows(len, fits && longest <= 128);
+    limit = p.few_rows = few_rows(len, hd, fits && longest <= 128, sixteens * kv.n_kv_heads <= zsa::device_cu_count());
     most[0] = most[1] = 0;
     for (int b = 0; b < batch; ++b) {
       const int64_t rows = (cu[b + 1] - cu[b]) * G;
@@ -176,14 +182,16 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
                              : !fits;
     l.tile = many ? zsa::kPagedManyRows : !matrix && max_rows > 16 && wide ? 32 : zsa::kPagedFewRows;
     l.tiles = static_cast<int>((max_rows + l.tile - 1) / l.tile);
-    int64_t workgroups = common ? l.tiles : 0;
+    int64_t workgroups = common ? l.tiles : 0, packed = common ? T * G : 0;
     for (int b = 0; b < batch && !common; ++b) {
       const int64_t rows = (cu[b + 1] - cu[b]) * G;
-      if (many == (matrix && rows > limit)) workgroups += (rows + l.tile - 1) / l.tile;
+      if (many != (matrix && rows > limit)) continue;
+      workgroups += (rows + l.tile - 1) / l.tile;
+      packed += rows;
     }
     l.waves = alone && !many ? zsa::paged_waves(matrix, kv.dtype, hd, l.tile, max_len, workgroups * kv.n_kv_heads) : 4;
-    l.chunk = zsa::paged_chunk(many, matrix, hd, max_len, workgroups * kv.n_kv_heads, !common && batch > 1,
-                               alone ? 0 : prefix > 0 ? 2 : 1, other, &l.splits);
+    l.chunk = zsa::paged_chunk(many, matrix, hd, max_len, workgroups * kv.n_kv_heads, packed * kv.n_kv_heads,
+                               !common && batch > 1, alone ? 0 : prefix > 0 ? 2 : 1, other, &l.splits);
     if (!many) other += workgroups * kv.n_kv_heads * hd * 2.0 * esize(kv.dtype) * max_len / 2 / 5e6;
     return l;
   };

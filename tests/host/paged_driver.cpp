@@ -39,7 +39,7 @@ int set_error(int code, const char* fmt, ...) {
 int device_cu_count() { return 256; }
 bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 32; }
 int paged_waves(bool, int, int, int, int, int64_t) { return 4; }
-int paged_chunk(bool many, bool, int, int max_len, int64_t workgroups, bool, int, double, int* splits) {
+int paged_chunk(bool many, bool, int, int max_len, int64_t workgroups, int64_t, bool, int, double, int* splits) {
   const int least = many ? 256 : 512, blocks = max_len > 0 ? (max_len + least - 1) / least : 1;
   const int want = workgroups > 64 ? 1 : blocks < 7 ? blocks : 7;
   const int per = (blocks + want - 1) / want;

@@ -190,6 +190,21 @@ def test_long_rows_in_one_split(dtype, H, kv, hd, batch, most, prefix):
     Batch(dtype, H, kv, hd, 64, [1] * batch, lens, prefix, seed=most).check(True, max_kv_len=most)
 
 
+@pytest.mark.parametrize("dtype,H,kv,hd,batch,n,most", [
+    ("bf16", 8, 2, 128, 4, 30, 1500),     # up to 120 packed rows in 16s
+    ("bf16", 8, 2, 128, 4, 30, 1600),     # the many-row kernel, a few of whose rows are there, in several splits
+    ("bf16", 6, 2, 64, 5, 10, 2900),      # two workgroups of 16 each
+    ("bf16", 6, 2, 64, 5, 10, 3200),
+    ("bf16", 4, 1, 32, 3, 200, 2500),     # four tiles of 256, the last in part
+    ("bf16", 4, 4, 128, 1, 300, 5000),
+    ("f32", 6, 2, 64, 3, 30, 1600),
+])
+def test_pieces_of_long_sequences(dtype, H, kv, hd, batch, n, most):
+    new = [n - 2 * b for b in range(batch)]
+    lens = [most - 211 * b for b in range(batch)]
+    Batch(dtype, H, kv, hd, 32, new, lens, seed=most + n).check(True, max_kv_len=most)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prefix_equals_the_same_rows_repeated(dtype):
     # the prefix cached once, against every sequence holding it as its own rows
