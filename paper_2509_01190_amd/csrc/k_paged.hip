@@ -524,6 +524,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD <= 6
 //  * The resource ends with the sequence, so rows behind it read as zeros.
 //  * The packed rows put the G query heads that share a key/value head into
 //    one workgroup: its tiles are read once for all of them.
+//  * A common prefix that the launch puts before the rows (HEAD) is filled up
+//    to 32 keys, masked in the one step that holds them.
 //  * P is rounded to bf16 for the second product, as there: half a step of
 //    each probability, which the sums of many average out.
 // 4 x 1024 new rows over up to 8024, 32 heads of 128 on 8, 360 us, 1.06 PFLOP/s
@@ -534,7 +536,7 @@ struct ManyShared {
   unsigned char tiles[NB * BUF > NW * WQ * OLD * 2 ? NB * BUF : NW * WQ * OLD * 2];
 };
 
-template <int HD, int QB, int NW>
+template <int HD, int QB, int NW, bool HEAD>
 __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, ManyShared<HD, QB, NW>& shared) {
   constexpr int WQ = 32 * QB, BQ = WQ * NW, BK = 64;
   constexpr int KK = HD / 16, CT = HD / 32, CPR = HD / 8;
@@ -556,8 +558,13 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
   const int half = lane >> 5, l32 = lane & 31;
   const int wq0 = i0 + wave * WQ;  // the wave's first packed row
   const float scale_log2 = a.scale * kLog2e;
+  // A common prefix in the same job (HEAD) comes first, as in few_rows
+  const int head = HEAD ? (a.head_len + 31) & ~31 : 0, end = head + sp.len;
   // keys that packed row i sees
-  auto seen = [&](int i) { return a.causal ? min(sp.first + min(i, sp.rows - 1) / a.G, sp.len) : sp.len; };
+  auto seen = [&](int i) {
+    const int n = a.causal ? min(sp.first + min(i, sp.rows - 1) / a.G, sp.len) : sp.len;
+    return HEAD ? head + max(n, 0) : n;
+  };
   const int k0 = split * a.chunk;
   const int kend = min(seen(i0 + BQ - 1), k0 + a.chunk);
   const int nt = max((kend - k0 + BK - 1) / BK, 0);
@@ -576,12 +583,18 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
   const char* pool = static_cast<const char*>(a.at.pool);
   // ids of the 64 pages from `idp` on, one a lane, and of the 64 after them
   // (the reads do not wait for the length: up to the table's end they go through)
-  const int most = a.at.max_pages - 1;
-  int idp = k0 >> a.at.shift;
-  auto read_ids = [&](int from) { return most >= 0 ? sp.table[min(from + lane, most)] : -1; };
+  // (with a prefix its pages' ids and then the sequence's, as one list)
+  const int most = a.at.max_pages - 1, hpages = HEAD ? (head + (1 << a.at.shift) - 1) >> a.at.shift : 0;
+  auto place = [&](int j) { return HEAD && j >= head ? hpages + ((j - head) >> a.at.shift) : j >> a.at.shift; };
+  int idp = place(k0);
+  auto read_ids = [&](int from) {
+    const int p = from + lane;
+    if (HEAD && p < hpages) return a.head_table[min(p, (a.head_len - 1) >> a.at.shift)];
+    return most >= 0 ? sp.table[min(p - hpages, most)] : -1;
+  };
   int ids = read_ids(idp), idn = read_ids(idp + 64);
   auto load_rows = [&](int j, uint32_t lds) {  // K and V of RPL rows from row j on
-    const int p = j >> a.at.shift;
+    const int p = place(j), left = (HEAD && j < head ? a.head_len : end) - j;
     if (p >= idp + 64) {
       asm volatile("" : "+v"(idn));  // waited for here
       ids = idn;
@@ -589,10 +602,10 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
       idn = read_ids(idp + 64);
     }
     const int page = __builtin_amdgcn_readlane(ids, p - idp);
-    const bool there = j < sp.len && page >= 0 && page < a.at.n_pages;
-    const uint32_t bytes = there ? static_cast<uint32_t>(min(sp.len - j, RPL)) * rowb - g * RB : 0u;
+    const bool there = left > 0 && page >= 0 && page < a.at.n_pages;
+    const uint32_t bytes = there ? static_cast<uint32_t>(min(left, RPL)) * rowb - g * RB : 0u;
     const char* at = pool + (there ? page : 0) * (a.at.page_stride * 2) +
-                     static_cast<uint32_t>(j & ((1 << a.at.shift) - 1)) * rowb + g * RB;
+                     static_cast<uint32_t>((HEAD && j >= head ? j - head : j) & ((1 << a.at.shift) - 1)) * rowb + g * RB;
     u32x4 kres = buffer_resource(at, bytes), vres = buffer_resource(at + rowb / 2, there ? bytes - rowb / 2 : 0u);
     // a load in asm may follow a vector instruction's write of its scalar operands by five states at least
     asm volatile("s_nop 4" : "+s"(kres), "+s"(vres));
@@ -665,10 +678,11 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
     };
     auto mask = [&](int u, f32x16_t (&s)[QB]) {
       const int j0 = k0 + 32 * u;
-      if (j0 + 32 <= wlim0) return;
+      const bool fill = HEAD && j0 < head && j0 + 32 > a.head_len;
+      if (j0 + 32 <= wlim0 && !fill) return;
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
-        int left = lim[qb] - j0 - 4 * half;  // keys from this lane's limit on are masked
+        int left = (fill ? a.head_len : lim[qb]) - j0 - 4 * half;  // keys from this lane's limit on are masked
         asm("" : "+v"(left));  // the comparisons stay here (hoisted, their masks fill the scalar registers)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
@@ -823,7 +837,7 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
   // through the product with its zero probability it has, and left a NaN.
   // Where the wave's tiles hold hidden keys and its results a NaN, its rows are
   // computed again, the second product on the vector ALU, key by key.
-  if (busy && wlim0 < min(sp.len, k0 + ntw * BK)) {
+  if (busy && wlim0 < min(end, k0 + ntw * BK)) {
     bool odd = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
@@ -833,10 +847,12 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
         for (int r = 0; r < 16; ++r) odd |= o[qb][ct][r] != o[qb][ct][r];
     if (__builtin_amdgcn_ballot_w64(odd) != 0) {
       auto row_of = [&](int j) {  // row j's keys, or null
-        const int page = j < sp.len ? sp.table[j >> a.at.shift] : -1;
+        const bool first = HEAD && j < head;
+        const int i = first ? j : j - head;
+        const int page = i < (first ? a.head_len : sp.len) ? (first ? a.head_table : sp.table)[i >> a.at.shift] : -1;
         return page < 0 || page >= a.at.n_pages
                    ? nullptr
-                   : pool + page * (a.at.page_stride * 2) + static_cast<uint32_t>(j & ((1 << a.at.shift) - 1)) * rowb + g * RB;
+                   : pool + page * (a.at.page_stride * 2) + static_cast<uint32_t>(i & ((1 << a.at.shift) - 1)) * rowb + g * RB;
       };
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
@@ -857,7 +873,8 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
           float mx = m;
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            if (j0 + 8 * (r >> 2) + 4 * half + (r & 3) >= lim[qb]) s[r] = -INFINITY;
+            const int j = j0 + 8 * (r >> 2) + 4 * half + (r & 3);
+            if (j >= lim[qb] || (HEAD && j < head && j >= a.head_len)) s[r] = -INFINITY;
             mx = fmaxf(mx, s[r] * scale_log2);
           }
           mx = half_swap_max(mx);
@@ -953,7 +970,7 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
 
 // The many-row kernel, and the few-row one's work in the same launch: its
 // workgroups fill the CUs that the first, longer ones leave.
-template <int HD, int QB, int NW>
+template <int HD, int QB, int NW, bool HEAD>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_many_kernel(PagedJobs many,
                                                                                                       PagedJobs few) {
   constexpr int GROUPS = NW / 4;
@@ -964,13 +981,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   if (blockIdx.x < many.blocks) {
     const int which = blockIdx.x >= many.first;
     const PagedAttention a = many.job[which];  // (a copy: what it holds stays in registers)
-    many_rows<HD, QB, NW>(a, blockIdx.x - (which ? many.first : 0), shared.many);
+    many_rows<HD, QB, NW, HEAD>(a, blockIdx.x - (which ? many.first : 0), shared.many);
   } else {
     const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
     const uint32_t block = (blockIdx.x - many.blocks) * GROUPS + group;
     const int which = block >= few.first;
     const PagedAttention a = few.job[which];
-    few_rows<HD, 4, false>(a, block - (which ? few.first : 0), block < few.blocks, threadIdx.x & 255, shared.few[group]);
+    few_rows<HD, 4, HEAD>(a, block - (which ? few.first : 0), block < few.blocks, threadIdx.x & 255, shared.few[group]);
   }
 }
 
@@ -1544,6 +1561,14 @@ int64_t paged_blocks(const PagedAttention& a, bool many) {
   return (many ? (pairs + 7) / 8 * 8 : pairs) * a.tiles;
 }
 
+template <bool HEAD>
+static hipError_t many_dispatch(hipStream_t s, int hd, const PagedJobs& many, const PagedJobs& few) {
+  const dim3 grid(many.blocks + (hd == 128 ? (few.blocks + 1) / 2 : few.blocks));
+  if (hd == 32) return launch(K_ATTENTION, paged_many_kernel<32, 2, 4, HEAD>, grid, dim3(256), 0, s, many, few);
+  if (hd == 64) return launch(K_ATTENTION, paged_many_kernel<64, 2, 4, HEAD>, grid, dim3(256), 0, s, many, few);
+  return launch(K_ATTENTION, paged_many_kernel<128, 1, 8, HEAD>, grid, dim3(512), 0, s, many, few);
+}
+
 hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention* few, int fews,
                                   const PagedAttention* many, int manys) {
   PagedJobs w[2] = {};
@@ -1557,13 +1582,8 @@ hipError_t launch_paged_attention(hipStream_t s, int dtype, const PagedAttention
     w[k].blocks = w[k].first + (n > 1 ? static_cast<uint32_t>(paged_blocks(job[1], k != 0)) : 0u);
   }
   const int hd = (manys > 0 ? many : few)[0].hd;
-  if (manys > 0) {
-    if (hd == 32)
-      return launch(K_ATTENTION, paged_many_kernel<32, 2, 4>, dim3(w[1].blocks + w[0].blocks), dim3(256), 0, s, w[1], w[0]);
-    if (hd == 64)
-      return launch(K_ATTENTION, paged_many_kernel<64, 2, 4>, dim3(w[1].blocks + w[0].blocks), dim3(256), 0, s, w[1], w[0]);
-    return launch(K_ATTENTION, paged_many_kernel<128, 1, 8>, dim3(w[1].blocks + (w[0].blocks + 1) / 2), dim3(512), 0, s, w[1], w[0]);
-  }
+  if (manys > 0)
+    return many[0].head_len > 0 ? many_dispatch<true>(s, hd, w[1], w[0]) : many_dispatch<false>(s, hd, w[1], w[0]);
   return few[0].head_len > 0 ? few_dispatch<true>(s, dtype, w[0]) : few_dispatch<false>(s, dtype, w[0]);
 }
 

@@ -457,7 +457,7 @@ struct PagedAttention {
   const int32_t* cu;          // null: all T rows are one sequence's (a common prefix)
   const int32_t* kv_len;      // null: max_len rows
   int max_len;                // rows from this one on are not read
-  const int32_t* head_table;  // pages of a common prefix that the few-row kernels put before the rows, and
+  const int32_t* head_table;  // pages of a common prefix that the kernels put before the rows, and
   int head_len;               // its rows (0: none)
   int T, B, H, G, hd;
   int causal;

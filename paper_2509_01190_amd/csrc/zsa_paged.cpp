@@ -117,7 +117,7 @@ struct Part {
   int tile, tiles;    // packed rows of a workgroup; of the longest sequence, how many of those
   int waves;          // of a few-row workgroup
   int chunk, splits;  // 0 splits: there are none
-  bool head;          // the common prefix goes before the sequences' rows
+  bool head;          // the common prefix goes before the sequences' rows, in the same workgroups
 };
 
 // The parts of the prefix come first, the others' after them, in the same places.
@@ -146,15 +146,19 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   // (what LDS holds of the few-row kernels' workgroups, a CU)
   const int resident = 512 / (hd * static_cast<int>(esize(kv.dtype)));
   const bool fits = sixteens * kv.n_kv_heads <= static_cast<int64_t>(zsa::device_cu_count()) * std::min(resident, 4);
-  // A short prefix is read once per sequence, in the same workgroups, where
-  // that is at most 32 MB, from the L2s, or with the own rows 160 and no parts are
-  // to join then (8 sequences of up to 41 rows behind 501, 12 heads of 64: 15.0 ->
-  // 10.7 us; 30 x 4 rows over up to 100 behind 700, 32 of 128 on 8, 98 MB, 22.1 ->
-  // 12.6, 60 over up to 1000 behind 500, 370 MB, 36.9 -> 44.6; fp32, 55 x 4 over 10
-  // behind 99, 49 MB, 40 -> 25.7).
-  const double again = static_cast<double>(batch) * prefix * row / (1 << 20);
-  const bool head = prefix > 0 && (again <= 32 || again * (1.0 + static_cast<double>(max_len) / prefix) <= 160) &&
-                    max_len < (1 << 29);
+  // A short prefix goes before the sequences' rows, in the same workgroups:
+  //  * those of few rows read it once per sequence, from the L2s, where that is at
+  //    most 32 MB, or with the own rows 160 and no parts are to join then (8
+  //    sequences of up to 41 rows behind 501, 12 heads of 64: 15.0 -> 10.7 us; 30 x 4
+  //    rows over up to 100 behind 700, 32 of 128 on 8, 98 MB, 22.1 -> 12.6, 60 over
+  //    up to 1000 behind 500, 370 MB, 36.9 -> 44.6; fp32, 55 x 4 over 10 behind 99,
+  //    49 MB, 40 -> 25.7);
+  //  * those of many rows take no part's bytes and no join for it, but are more
+  //    than the rows of all together would be (`more` us): 5 of up to 757 rows
+  //    behind 226, 8 heads of 128 on 1, 77.6 -> 36.3; 8 of up to 200 behind 1000, 32
+  //    of 128 on 8, 56.0 -> 42.2, behind 3000 95.2 -> 91.4; 1 of 300 behind 300, 12 of
+  //    64, 17.2 -> 18.5.
+  const bool head = prefix > 0 && max_len < (1 << 29) && prefix < (1 << 29);
   const int whole = head ? (prefix + 31) / 32 * 32 + max_len : 0;
   int limit;
   int64_t most[2];
@@ -169,7 +173,8 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
   };
   double other = 0;  // us of the few-row work: its cached rows, half the longest each, at 5 TB/s
   const int max_own = max_len;
-  auto part = [&](bool many, int64_t max_rows, int max_len, bool common, bool alone) {
+  // (`beside` as in paged_chunk)
+  auto part = [&](bool many, int64_t max_rows, int max_len, bool common, int beside) {
     Part l{};
     l.many = many;
     // fp32: 32 rows a workgroup cost less than twice 16, and more than 16 on
@@ -189,28 +194,44 @@ Plan plan_of(const zsa_paged_kv& kv, int H, int batch, const int32_t* cu, int ma
       workgroups += (rows + l.tile - 1) / l.tile;
       packed += rows;
     }
-    l.waves = alone && !many ? zsa::paged_waves(matrix, kv.dtype, hd, l.tile, max_len, workgroups * kv.n_kv_heads) : 4;
+    l.waves = beside == 0 && !many ? zsa::paged_waves(matrix, kv.dtype, hd, l.tile, max_len, workgroups * kv.n_kv_heads) : 4;
     l.chunk = zsa::paged_chunk(many, matrix, hd, max_len, workgroups * kv.n_kv_heads, packed * kv.n_kv_heads,
-                               !common && batch > 1, alone ? 0 : prefix > 0 ? 2 : 1, other, &l.splits);
+                               !common && batch > 1, beside, other, &l.splits);
     if (!many) other += workgroups * kv.n_kv_heads * hd * 2.0 * esize(kv.dtype) * max_len / 2 / 5e6;
     return l;
   };
   if (head) {
     sort(whole);
-    if (most[1] == 0) {
-      p.few = part(false, most[0], whole, false, true);
-      p.few.head = true;
-      if (again <= 32 || p.few.splits == 1) return p;
-      p.few = Part{};
+    int64_t fews = 0, tiles = 0, many_rows = 0;
+    for (int b = 0; b < batch; ++b) {
+      const int64_t rows = (cu[b + 1] - cu[b]) * G;
+      const bool many = matrix && rows > limit;
+      fews += !many && rows > 0;
+      if (!many) continue;
+      tiles += (rows + zsa::kPagedManyRows - 1) / zsa::kPagedManyRows;
+      many_rows += rows;
+    }
+    const double again = static_cast<double>(fews) * prefix * row / (1 << 20);
+    const double own = again / prefix * max_len;
+    const int64_t common = (T * G + zsa::kPagedManyRows - 1) / zsa::kPagedManyRows;
+    const double more = static_cast<double>(std::max<int64_t>(tiles - common, 0)) * kv.n_kv_heads * prefix / 64 * 1.5 / zsa::device_cu_count();
+    const double parts = 4 + 2.0 * many_rows * kv.n_kv_heads * hd * 8 / 2e6;
+    if ((again <= 32 || again + own <= 160) && (tiles == 0 || more <= parts)) {
+      p.few = p.many = Part{};
+      if (most[0] > 0) p.few = part(false, most[0], whole, false, most[1] > 0);
+      if (most[1] > 0) p.many = part(true, most[1], whole, false, 0);
+      p.few.head = p.many.head = true;
+      if (again <= 32 || p.own() == 1) return p;
+      p.few = p.many = Part{};
       other = 0;
     }
   }
   sort(max_len);
-  if (most[0] > 0) p.few = part(false, most[0], max_len, false, prefix == 0 && most[1] == 0);
-  if (most[1] > 0) p.many = part(true, most[1], max_len, false, prefix == 0);
+  if (most[0] > 0) p.few = part(false, most[0], max_len, false, prefix > 0 ? 2 : most[1] > 0);
+  if (most[1] > 0) p.many = part(true, most[1], max_len, false, prefix > 0 ? 2 : 0);
   if (prefix > 0) {
     // (one launch takes one width of tiles)
-    p.prefix = part(matrix && !few_prefix(hd, kv.n_kv_heads, T * G, prefix), T * G, prefix, true, false);
+    p.prefix = part(matrix && !few_prefix(hd, kv.n_kv_heads, T * G, prefix), T * G, prefix, true, 2);
     if (!matrix && p.few.splits > 0 && p.few.tile != p.prefix.tile) {
       p.few.tile = p.prefix.tile;
       p.few.tiles = static_cast<int>((most[0] + p.few.tile - 1) / p.few.tile);

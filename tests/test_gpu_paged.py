@@ -217,12 +217,23 @@ def test_prefix_equals_the_same_rows_repeated(dtype):
     b.compare(out2, lse2, *b.oracle(True))
 
 
+@pytest.mark.parametrize("H,kv,hd", [(4, 2, 64), (4, 1, 128), (2, 2, 32)])
+@pytest.mark.parametrize("page", [16, 256])
+@pytest.mark.parametrize("prefix", [1, 31, 33, 64, 1100])
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompts_behind_a_prefix(H, kv, hd, page, prefix, causal):
+    # rows for the many-row kernel, which takes the prefix's with them; some that see no row of their own
+    new = [300, 1, 0, 270, 150, 2]
+    lens = [300, 40, 0, 333, 100, 0]
+    Batch("bf16", H, kv, hd, page, new, lens, prefix, seed=prefix + hd).check(causal)
+
+
 @pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 128), ("bf16", 32), ("f32", 64)])
-@pytest.mark.parametrize("n", [1, 40, 300])
-def test_values_that_are_not_finite(dtype, hd, n):
+@pytest.mark.parametrize("n,prefix", [(1, 0), (40, 0), (300, 0), (1, 37), (40, 37), (300, 37)])
+def test_values_that_are_not_finite(dtype, hd, n, prefix):
     # The last new row holds an infinity and the one before it a NaN: the
     # rows before them do not see them
-    b = Batch(dtype, 4, 2, hd, 16, [n, 1], [n + 150, 9], seed=n)
+    b = Batch(dtype, 4, 2, hd, 16, [n, 1], [n + 150, 9], prefix, seed=n)
     size, m = b.page, n + 150
     for row, value in ((m - 1, float("inf")), (m - 2, float("nan"))):
         if row >= 150:
@@ -235,7 +246,7 @@ def test_values_that_are_not_finite(dtype, hd, n):
     assert rows.sum() >= n - 1
     got, p = f64(out), half_step(b.dtype)
     err = np.abs(got[rows] - ref[rows])
-    ds = (2 * (hd + 8) * U32 * (mag.max() + 4) + 2 * (m + 8) * U32 + p)
+    ds = (2 * (hd + 8) * U32 * (mag.max() + 4) + 2 * (m + prefix + 8) * U32 + p)
     assert (err <= ds * mags[rows] + p * (1 + p) * np.abs(ref[rows]) + 1e-30).all()
 
 
