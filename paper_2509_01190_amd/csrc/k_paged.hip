@@ -1381,6 +1381,9 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const float2* __restric
 
 template <typename T, int HD, int W, bool HEAD>
 hipError_t f32_launch(hipStream_t s, const PagedJobs& jobs) {
+  if constexpr (W == 16)
+    if (jobs.job[0].waves == 1)
+      return launch(K_ATTENTION, paged_f32_kernel<T, HD, W, 1, HEAD>, dim3(jobs.blocks), dim3(64), 0, s, jobs);
   if constexpr (W == 16 && HD * sizeof(T) <= 256)
     if (jobs.job[0].waves == 8)
       return launch(K_ATTENTION, paged_f32_kernel<T, HD, W, 8, HEAD>, dim3(jobs.blocks), dim3(512), 0, s, jobs);
@@ -1452,8 +1455,10 @@ hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a) {
 bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 32; }
 
 // Waves of a few-row workgroup: eight where the workgroups do not fill the CUs
-// and every wave has more than two steps of 32 keys otherwise.
+// and every wave has more than two steps of 32 keys otherwise; in fp32 one where
+// they are more and have two steps each.
 int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t workgroups) {
+  if (!matrix && tile == 16 && max_len <= 64 && workgroups > device_cu_count()) return 1;
   const bool can = matrix || (tile == 16 && hd * (dtype == 1 ? 2 : 4) <= 256);
   return can && max_len > 256 && workgroups <= device_cu_count() ? 8 : 4;
 }
