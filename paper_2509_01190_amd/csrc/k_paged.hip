@@ -1403,6 +1403,8 @@ hipError_t f32_dispatch(hipStream_t s, const PagedJobs& jobs) {
 
 template <int HD, bool HEAD>
 hipError_t few_launch(hipStream_t s, const PagedJobs& jobs) {
+  if (jobs.job[0].waves == 1)
+    return launch(K_ATTENTION, paged_few_kernel<HD, 1, HEAD>, dim3(jobs.blocks), dim3(64), 0, s, jobs);
   if (jobs.job[0].waves == 8)
     return launch(K_ATTENTION, paged_few_kernel<HD, 8, HEAD>, dim3(jobs.blocks), dim3(512), 0, s, jobs);
   return launch(K_ATTENTION, paged_few_kernel<HD, 4, HEAD>, dim3(jobs.blocks), dim3(256), 0, s, jobs);
@@ -1455,12 +1457,16 @@ hipError_t launch_paged_append(hipStream_t s, int dtype, const PagedAppend& a) {
 bool paged_matrix(int dtype, int hd) { return dtype == 1 && hd >= 32; }
 
 // Waves of a few-row workgroup: eight where the workgroups do not fill the CUs
-// and every wave has more than two steps of 32 keys otherwise; in fp32 one where
-// they are more and have two steps each.
+// and every wave has more than two steps of 32 keys otherwise; one where short
+// workgroups are many, and more of them run on a CU then (with four / one, us: 47
+// sequences of up to 30 rows, 32 heads of 128, 14.6 / 8.9, of 250 27.9 / 25.9, 12 of
+// 120 8.2 / 8.8; fp32, 47 of 30 36.6 / 16.4, 40 of 60, 32 of 128 on 8, 14.7 / 12.2,
+// 60 of 250 27.3 / 30.9).
 int paged_waves(bool matrix, int dtype, int hd, int tile, int max_len, int64_t workgroups) {
-  if (!matrix && tile == 16 && max_len <= 64 && workgroups > device_cu_count()) return 1;
+  const int cus = device_cu_count();
+  if (tile == 16 && ((max_len <= 256 && workgroups * 2 >= cus * 5) || (!matrix && max_len <= 64 && workgroups > cus))) return 1;
   const bool can = matrix || (tile == 16 && hd * (dtype == 1 ? 2 : 4) <= 256);
-  return can && max_len > 256 && workgroups <= device_cu_count() ? 8 : 4;
+  return can && max_len > 256 && workgroups <= cus ? 8 : 4;
 }
 
 // Keys that a few-row workgroup takes in one split (see paged_chunk).

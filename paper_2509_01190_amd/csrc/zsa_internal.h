@@ -463,7 +463,7 @@ struct PagedAttention {
   int causal;
   float scale;
   int tile, tiles;            // packed rows of a workgroup; of the longest sequence, how many of those
-  int waves;                  // of a few-row workgroup: 4 or 8
+  int waves;                  // of a few-row workgroup: 1, 4 or 8
   int once;                   // the call's cached rows outgrow the last-level cache: read each past it
   int few_rows;               // a few-row launch takes the sequences of up to so many packed rows, a many-row one the others
   int chunk, splits;          // keys a split takes, a multiple of 128; splits

@@ -205,6 +205,16 @@ def test_pieces_of_long_sequences(dtype, H, kv, hd, batch, n, most):
     Batch(dtype, H, kv, hd, 32, new, lens, seed=most + n).check(True, max_kv_len=most)
 
 
+@pytest.mark.parametrize("dtype,H,kv,hd", [("bf16", 16, 16, 64), ("bf16", 16, 16, 128), ("bf16", 16, 16, 32),
+                                           ("bf16", 16, 16, 16), ("f32", 16, 16, 64), ("f32", 16, 16, 128)])
+@pytest.mark.parametrize("most,prefix", [(33, 0), (64, 0), (200, 0), (20, 13), (60, 100)])
+def test_many_short_sequences(dtype, H, kv, hd, most, prefix):
+    # more than two workgroups a CU
+    new = [1 + (b % 5 == 0) for b in range(45)]
+    lens = [(most * (b % 9)) // 8 for b in range(45)]
+    Batch(dtype, H, kv, hd, 16, new, lens, prefix, seed=most + hd).check(True, max_kv_len=most)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prefix_equals_the_same_rows_repeated(dtype):
     # the prefix cached once, against every sequence holding it as its own rows
