@@ -477,7 +477,8 @@ struct PagedAttention {
 };
 constexpr int kPagedManyRows = 256, kPagedFewRows = 16;  // packed rows of a workgroup (the fp32 kernel: 16 or 32)
 bool paged_matrix(int dtype, int hd);  // the bf16 matrix kernels take these heads: one for few rows, one for many
-// keys a split of up to max_len rows takes, and how many splits that makes; joined: rows have other parts anyway; other: us of
+// keys a split of up to max_len rows takes, and how many splits that makes, for `workgroups` of `rows` packed rows of all
+// key/value heads. beside: 1 jobs of other sequences, 2 a common prefix's, so that rows have other parts anyway; other: us of
 // few-row work beside many-row workgroups
 int paged_chunk(bool many, bool matrix, int hd, int max_len, int64_t workgroups, int64_t rows, bool ragged, int beside, double other,
                 int* splits);
