@@ -97,12 +97,12 @@ size_t parts_bytes(int64_t parts, int64_t rows, int hd) {
 // on 1, 12.1 / 19.3; 3 of 60 to 100 rows over up to 600, 12 of 64, 8.4 / 19.0; 12 of
 // 20 new rows over up to 1320, 24 of 64 on 8, 17.4 / 21.9; with more than run at
 // once it loses (25 of 10 to 20 rows over up to 920, 32 of 128 on 8, 35.1 / 24.7).
-// Two over up to 3072 in heads below 128 and at most one a CU (`one`): 12 of 8 new
+// Two over up to 3040 in heads below 128 and at most one a CU (`one`): 12 of 8 new
 // rows, 24 of 64 on 8, 18.6 / 22.5; 40, with more, 68 / 59; 12, 32 of 128 on 8, 37.4
 // / 34.7.
 int few_rows(int max_len, int hd, bool fits, bool one) {
   if (fits && max_len <= 1536) return 128;
-  return max_len <= (one && hd < 128 ? 3072 : 1024) ? 32 : 16;
+  return max_len <= (one && hd < 128 ? 3040 : 1024) ? 32 : 16;
 }
 bool few_prefix(int hd, int kv_heads, int64_t rows, int prefix) {
   const int64_t workgroups = (rows + 15) / 16 * kv_heads;
