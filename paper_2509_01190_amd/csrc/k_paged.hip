@@ -394,14 +394,16 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
         for (int r = 0; r < 4; ++r) o[ct][r] *= alpha;
       m_run = m_new;
     }
-    const float m_use = m_run == -INFINITY ? 0.f : m_run * scale_log2;
+    // (the difference first: where a scaled score is rounded by many units of an
+    // exponential, a product's rounding would be left in it)
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
     u32x4 hi, lo;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 4; r += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t][r], scale_log2, -m_use));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[t][r + 1], scale_log2, -m_use));
+        const float p0 = __builtin_amdgcn_exp2f((s[t][r] - m_use) * scale_log2);
+        const float p1 = __builtin_amdgcn_exp2f((s[t][r + 1] - m_use) * scale_log2);
         l_run += p0 + p1;
         const uint32_t w = pack_bf16x2(p0, p1);
         hi[2 * t + (r >> 1)] = w;
@@ -440,7 +442,7 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
 #pragma unroll
     for (int r = 0; r < 4; ++r) odd |= o[ct][r] != o[ct][r];
   if (__builtin_amdgcn_ballot_w64(odd && l_run == l_run) != 0) {
-    const float m_use = m_run == -INFINITY ? 0.f : m_run * scale_log2;
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) o[ct] = zero;
 #pragma unroll 1
@@ -456,7 +458,7 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
           s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k), qf[kk], kk == 0 ? zero : s[t], 0, 0, 0);
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], scale_log2, -m_use));
+        for (int r = 0; r < 4; ++r) s[t][r] = __builtin_amdgcn_exp2f((s[t][r] - m_use) * scale_log2);
       }
 #pragma unroll
       for (int kk = 0; kk < 32; ++kk) {

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from tests.helpers import f64
-from tests.test_gpu_paged import Batch
+from tests.test_gpu_paged import U32, Batch
 
 pytestmark = pytest.mark.gpu
 
@@ -33,6 +33,7 @@ TYPES = [("bf16", 32), ("bf16", 64), ("bf16", 128), ("bf16", 16), ("f32", 64)]
 CALLS = [([1, 1], [40, 9], 0), ([1, 1], [1, 33], 0), ([1], [9000], 0), ([1] * 48, [30] * 48, 0),
          ([40, 3], [190, 64], 0), ([300, 1], [450, 20], 0), ([1, 1], [40, 9], 37), ([40, 3], [60, 64], 37),
          ([300, 1], [320, 20], 100), ([1, 20], [40, 50], 9000)]
+FEW = [c for c in CALLS if len(c[0]) < 9 and max(c[0]) < 300 and c[2] < 9000]  # the few-row kernels'
 
 
 @pytest.mark.parametrize("dtype,hd", TYPES)
@@ -57,3 +58,45 @@ def test_infinite_values(dtype, hd, new, lens, prefix, causal):
     assert n == 1 or np.isnan(ref[new[0] - 1, 7])
     if prefix:
         assert np.isposinf(ref[:, 9]).all() and np.isneginf(ref[:, 3 * hd + 9]).all()
+
+
+def margins(b, causal):
+    """Of every row and head: how far its largest score is above the next."""
+    pool, q, G, kvd = f64(b.pool), f64(b.q).reshape(b.cu[-1], b.H, b.hd), b.H // b.kv, b.kv * b.hd
+    out = np.full((b.H, b.cu[-1]), np.inf)
+    for s, n in enumerate(b.lens):
+        own = b.cu[s + 1] - b.cu[s]
+        rows = [pool[ids[r // b.page], r % b.page, :kvd] for ids, m in ((b.head, b.prefix), (b.table[s], n)) for r in range(m)]
+        k = np.array(rows).reshape(-1, b.kv, b.hd)
+        for r in range(own):
+            seen = b.prefix + (n - own + r + 1 if causal else n)
+            for h in range(b.H):
+                x = np.sort(k[:seen, h // G] @ q[b.cu[s] + r, h])[::-1] * b.hd ** -0.5
+                if len(x) > 1:
+                    out[h, b.cu[s] + r] = x[0] - x[1]
+    return out
+
+
+@pytest.mark.parametrize("dtype,hd", TYPES)
+@pytest.mark.parametrize("new,lens,prefix", FEW + [([1, 1], [40, 50], 9000)])
+@pytest.mark.parametrize("power", [14, 22, 50])
+@pytest.mark.parametrize("negative", [False, True])
+def test_far_scores(dtype, hd, new, lens, prefix, power, negative):
+    # Scores of 2^28, 2^44 and 2^100 times the ordinary ones, whose roundings are
+    # many units of an exponential: every row takes the value of its first key.
+    b = Batch(dtype, 4, 2, hd, 16, new, lens, prefix, seed=power + new[0])
+    b.q.mul_(2.0 ** power)
+    keys = b.pool[..., :2 * hd]
+    if negative:  # all of them below zero
+        b.q.abs_()
+        keys.abs_().neg_()
+    keys.mul_(2.0 ** power)
+    out, lse = b.run(True)
+    ref, rlse, _, mag = b.oracle(True)
+    err = (hd + 8) * U32 * (mag + 1)  # of a score: hd products and their sum, its scale
+    # the next key's probability is below 2^-140 whatever the roundings do: none is left of it in 32 bits
+    clear = margins(b, True) > 4 * err + 100
+    assert clear.mean() > 0.5, clear.mean()
+    rows = clear.T[:, :, None].repeat(hd, 2).reshape(ref.shape)
+    assert np.array_equal(f64(out)[rows], ref[rows])
+    assert (np.abs(f64(lse) - rlse)[clear] <= (err + 4 * U32 * np.abs(rlse))[clear]).all()
