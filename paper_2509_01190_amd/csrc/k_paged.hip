@@ -31,6 +31,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNoReference = -3.402823466e38f;  // a reference maximum of no key: the lowest number, from which an infinite score is infinitely far
 
 // ---------------------------------------------------------------------------
 // append
@@ -652,7 +653,7 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     l_run[qb] = 0.f;
-    mu[qb] = -1e30f;
+    mu[qb] = kNoReference;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -827,7 +828,7 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
       mask(1, sb);
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb)
-        mu[qb] = fmaxf(fmaxf(row_max(sa[qb]), row_max(sb[qb])) * scale_log2, -1e30f);
+        mu[qb] = fmaxf(fmaxf(row_max(sa[qb]), row_max(sb[qb])) * scale_log2, kNoReference);
       step(0, bc, 1, bp, 1, sa, sb, std::true_type());
     }
     if (nt > 2) load_tile(2, bp);
@@ -862,21 +863,28 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) l_run[qb] = half_swap_sum(l_run[qb]);
   // A value that is not finite must not reach a row that does not see its key;
-  // through the product with its zero probability it has, and left a NaN.
-  // Where the wave's tiles hold hidden keys and its results a NaN, its rows are
-  // computed again, the second product on the vector ALU, key by key.
-  if (busy && wlim0 < min(end, k0 + ntw * BK)) {
+  // through the product with its zero probability it has, and left a NaN. And a
+  // reference of 2^27 and more is rounded by 8 and more, which is left in the
+  // exponents of a row, from 128 on as zeros and infinities. Where the wave's
+  // tiles hold hidden keys and its results a NaN, or its references are that far,
+  // its rows are computed again: the scores' difference to the maximum before
+  // its scale, the second product on the vector ALU, key by key.
+  if (busy) {
     bool odd = false;
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
+    for (int qb = 0; qb < QB; ++qb) odd |= fabsf(mu[qb]) >= 0x1p27f && mu[qb] != kNoReference;
+    if (wlim0 < min(end, k0 + ntw * BK)) {
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
+      for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) odd |= o[qb][ct][r] != o[qb][ct][r];
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) odd |= o[qb][ct][r] != o[qb][ct][r];
+    }
     if (__builtin_amdgcn_ballot_w64(odd) != 0) {
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
-        float m = -1e30f, l = 0.f;
+        float m = kNoReference, l = 0.f;  // of the raw scores
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -895,10 +903,10 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
           for (int r = 0; r < 16; ++r) {
             const int j = j0 + 8 * (r >> 2) + 4 * half + (r & 3);
             if (j >= lim[qb] || (HEAD && j < head && j >= a.head_len)) s[r] = -INFINITY;
-            mx = fmaxf(mx, s[r] * scale_log2);
+            mx = fmaxf(mx, s[r]);
           }
           mx = half_swap_max(mx);
-          const float alpha = __builtin_amdgcn_exp2f(m - mx);
+          const float alpha = __builtin_amdgcn_exp2f((m - mx) * scale_log2);
           m = mx;
           l *= alpha;
 #pragma unroll
@@ -908,7 +916,7 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
           float part = 0.f;
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale_log2, -m));
+            s[r] = __builtin_amdgcn_exp2f((s[r] - m) * scale_log2);
             part += s[r];
           }
           l += half_swap_sum(part);
@@ -931,7 +939,7 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
             }
           }
         }
-        mu[qb] = m;
+        mu[qb] = m * scale_log2;
         l_run[qb] = l;
       }
     }

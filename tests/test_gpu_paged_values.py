@@ -33,6 +33,7 @@ TYPES = [("bf16", 32), ("bf16", 64), ("bf16", 128), ("bf16", 16), ("f32", 64)]
 CALLS = [([1, 1], [40, 9], 0), ([1, 1], [1, 33], 0), ([1], [9000], 0), ([1] * 48, [30] * 48, 0),
          ([40, 3], [190, 64], 0), ([300, 1], [450, 20], 0), ([1, 1], [40, 9], 37), ([40, 3], [60, 64], 37),
          ([300, 1], [320, 20], 100), ([1, 20], [40, 50], 9000)]
+MANY = [([300, 1], [450, 20], 0), ([300, 1], [320, 20], 100), ([1, 20], [40, 50], 9000), ([200], [3000], 0)]
 FEW = [c for c in CALLS if len(c[0]) < 9 and max(c[0]) < 300 and c[2] < 9000]  # the few-row kernels'
 
 
@@ -78,7 +79,7 @@ def margins(b, causal):
 
 
 @pytest.mark.parametrize("dtype,hd", TYPES)
-@pytest.mark.parametrize("new,lens,prefix", FEW + [([1, 1], [40, 50], 9000)])
+@pytest.mark.parametrize("new,lens,prefix", FEW + [([1, 1], [40, 50], 9000)] + MANY)
 @pytest.mark.parametrize("power", [14, 22, 50])
 @pytest.mark.parametrize("negative", [False, True])
 def test_far_scores(dtype, hd, new, lens, prefix, power, negative):
