@@ -23,6 +23,7 @@ SOURCES = [
     "zsa_api.cpp",
     "zsa_static.cpp",
     "zsa_paged.cpp",
+    "zsa_paged_split.cpp",
     "k_norm.hip",
     "k_gemm.hip",
     "k_attn.hip",
