@@ -101,3 +101,44 @@ def test_far_scores(dtype, hd, new, lens, prefix, power, negative):
     rows = clear.T[:, :, None].repeat(hd, 2).reshape(ref.shape)
     assert np.array_equal(f64(out)[rows], ref[rows])
     assert (np.abs(f64(lse) - rlse)[clear] <= (err + 4 * U32 * np.abs(rlse))[clear]).all()
+
+
+def rounded(x):
+    return torch.from_numpy(np.asarray(x)).to(torch.bfloat16).double().numpy()
+
+
+@pytest.mark.parametrize("dtype,hd", TYPES)
+@pytest.mark.parametrize("length,far", [(2, False), (40, False), (40, True), (700, True), (9000, True)])
+@pytest.mark.parametrize("prefix", [0, 20])
+def test_probabilities_of_few_rows_have_16_bits(dtype, hd, length, far, prefix):
+    # Two keys count, with probabilities in the ratio 1 to exp(-x), in one tile or
+    # far apart; their values are 1 and the ratio in 8 bits, and of two signs, so
+    # that the sum is what the ratio has beyond 8 bits.
+    B, n = 24, 1
+    b = Batch(dtype, 4, 2, hd, 16, [n] * B, [length] * B, prefix, seed=length)
+    x = (1 + np.arange(B)) / 16.0
+    last = length - 1 if far else 1
+    one, ratio = torch.ones(()), torch.from_numpy(rounded(np.exp(-x)))
+    for ids in (b.table.reshape(-1), b.head):
+        b.pool[torch.from_numpy(ids.astype(np.int64)).to(b.pool.device)] = 0.0
+    keys, values = b.pool[..., :2 * hd].view(*b.pool.shape[:2], 2, hd), b.pool[..., 2 * hd:]
+    keys[..., 0] = -30000.0        # the others': nothing is left of them in 32 bits
+    for s in range(B):
+        for row, score, value in ((0, 0.0, -ratio[s]), (last, -x[s], one)):
+            page, slot = int(b.table[s, row // 16]), row % 16
+            keys[page, slot, :, 0] = score
+            values[page, slot] = value.item()
+    b.q.zero_()
+    b.q.view(B, 4, hd)[..., 0] = hd ** 0.5 if hd in (16, 64) else 8.0
+    scale = None if hd in (16, 64) else 0.125
+    out, lse = b.run(True, scale=scale)
+    ref, rlse, size, _ = b.oracle(True, scale=scale)
+    # A score has one product, exact, and the scale's rounding and its own; an
+    # exponential, the sums of two terms, a quotient: 12 roundings of 2^-24 (a
+    # prefix's keys add zeros). Two bf16 numbers: half a step of a half step.
+    p = 0.0 if dtype == "f32" or hd == 16 else 2.0 ** -16
+    tol = ((2 * x.max() + 12) * U32 + p) * size + torch.finfo(b.dtype).eps / 2 * np.abs(ref)
+    assert (np.abs(f64(out) - ref) <= tol).all(), (np.abs(f64(out) - ref) / tol).max()
+    assert (np.abs(f64(lse) - rlse) <= 16 * U32).all()
+    # with probabilities of 8 bits most rows would be beyond that
+    assert (np.abs(ref) > 4 * tol).mean() > 0.7
