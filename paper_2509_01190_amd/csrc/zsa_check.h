@@ -19,8 +19,9 @@ inline int check_seqs(int32_t batch, const int32_t* cu_host, const int32_t* cu_d
   if (cu_host[0] != 0) return set_error(ZSA_ESHAPE, "cu[0] = %d, must be 0", cu_host[0]);
   int32_t ml = 0;
   for (int b = 0; b < batch; ++b) {
+    // (before the difference: between offsets below 0 it may not fit)
+    if (cu_host[b + 1] < cu_host[b]) return set_error(ZSA_ESHAPE, "cu not monotone at sequence %d", b);
     const int32_t len = cu_host[b + 1] - cu_host[b];
-    if (len < 0) return set_error(ZSA_ESHAPE, "cu not monotone at sequence %d", b);
     if (len > ml) ml = len;
   }
   *total = cu_host[batch];

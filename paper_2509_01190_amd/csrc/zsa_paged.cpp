@@ -416,6 +416,8 @@ size_t zsa_paged_attention_workspace_size(const zsa_paged_kv* kv, int32_t n_head
       n_heads % kv->n_kv_heads != 0 || max_kv_len < 0 || prefix_len < 0 || max_kv_len > (1 << 30) ||
       prefix_len > (1 << 30) || check_head_dim(kv->head_dim) != ZSA_OK || check_dtype(kv->dtype) != ZSA_OK)
     return 0;  // (the call itself refuses these)
+  for (int b = 0; b < batch; ++b)
+    if (cu_host[b + 1] < cu_host[b]) return 0;
   const int T = cu_host[batch];
   if (T <= 0) return 0;
   const Plan p = plan_of(*kv, n_heads, batch, cu_host, max_kv_len, prefix_len);
