@@ -211,8 +211,10 @@ class Seqs:
     @classmethod
     def wrap(cls, cu, cu_dev: torch.Tensor) -> "Seqs":
         """Offsets that the caller holds on both sides already: ``cu`` on the
-        host, ``cu_dev`` the same int32 values on the device."""
-        host = _host_i32(cu)
+        host (copied), ``cu_dev`` the same int32 values on the device (kept)."""
+        host = np.array(cu, dtype=np.int32)
+        if host.ndim != 1 or host.size == 0:
+            raise ValueError("cu must be the offsets of a batch, one more than its sequences")
         if cu_dev.dtype != torch.int32 or not cu_dev.is_contiguous() or cu_dev.numel() != len(host):
             raise ValueError("cu_dev must hold the host's offsets as contiguous int32")
         return cls._of(host, cu_dev)

@@ -2,7 +2,9 @@
 offsets hold (no GPU)."""
 import ctypes
 
+import numpy as np
 import pytest
+import torch
 
 from paper_2509_01190_amd import zsa
 from tests.test_paged_cpu import append, attend, cu
@@ -16,3 +18,21 @@ def test_offsets_that_fall_are_refused(offs):
     h, c = cu(*offs), zsa.PagedKvStruct(page_stride=4096, n_pages=8, page_size=16, max_pages=4, n_kv_heads=2, head_dim=64,
                                         dtype=zsa.BF16)
     assert zsa.lib().zsa_paged_attention_workspace_size(ctypes.byref(c), 4, len(offs) - 1, zsa._hp32(h), 64, 40000) == 0
+
+
+def test_wrapped_offsets_are_the_calls_own():
+    # the rows that a call checks its tensors for and those that the library is
+    # given are the same, whatever the caller does with the array afterwards
+    host = np.array([0, 1, 3], dtype=np.int32)
+    seqs = zsa.Seqs.wrap(host, torch.tensor([0, 1, 3], dtype=torch.int32))
+    pointer = seqs.host_ptr()
+    host[1:] = 100, 3000
+    assert seqs.total == 3 and seqs.lengths == [1, 2]
+    assert [pointer[i] for i in range(3)] == [0, 1, 3] == [int(c) for c in seqs.host]
+
+
+@pytest.mark.parametrize("cu", [[], [[0, 1], [1, 2]]])
+def test_wrapped_offsets_that_are_none(cu):
+    dev = torch.tensor(cu, dtype=torch.int32).reshape(-1)
+    with pytest.raises(ValueError):
+        zsa.Seqs.wrap(cu, dev)
