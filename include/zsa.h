@@ -436,7 +436,7 @@ typedef struct zsa_paged_kv {
  *           below 0 or beyond the table is not stored)
  *   pos     [T] int32 device: the rows' positions; NULL: stored as they are
  *   q       NULL, or the same rows' queries, n_heads heads: rotated to q_out
- *           (which may be q itself)
+ *           (which may be q itself, with its stride)
  * No two of a call's rows may go to one cached row. T = 0 launches nothing;
  * T stays below 2^24.
  */

@@ -376,6 +376,8 @@ int zsa_paged_append(void* stream, const zsa_paged_kv* kv, const void* k, int64_
     const int64_t width = static_cast<int64_t>(n_heads) * kv->head_dim;
     CHECK(check_stride(kv->dtype, q_stride, width, "q_stride"));
     CHECK(check_stride(kv->dtype, q_out_stride, width, "q_out_stride"));
+    if (q_out == q && q_out_stride != q_stride && T > 1)
+      return set_error(ZSA_ESHAPE, "q_out is q with another stride: %lld, %lld", (long long)q_out_stride, (long long)q_stride);
   }
   if (pos != nullptr && !(rope_theta > 0.f)) return set_error(ZSA_EINVAL, "rope_theta <= 0");
   if (T > 0 && kv_len == nullptr) return set_error(ZSA_EINVAL, "kv_len is NULL");

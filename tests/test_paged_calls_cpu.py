@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2509_01190_amd import zsa
-from tests.test_paged_cpu import append, attend, cu
+from tests.test_paged_cpu import PTR, append, attend, cu
 
 
 @pytest.mark.parametrize("offs", [(0, 2 ** 31 - 1, -2 ** 31), (0, -2 ** 31), (0, 1, -1), (0, 2 ** 31 - 1, -2)])
@@ -36,3 +36,10 @@ def test_wrapped_offsets_that_are_none(cu):
     dev = torch.tensor(cu, dtype=torch.int32).reshape(-1)
     with pytest.raises(ValueError):
         zsa.Seqs.wrap(cu, dev)
+
+
+def test_queries_rotated_in_place_keep_their_stride():
+    # with another one a row would be written before it is read
+    q = dict(q=PTR[2], qs=512, H=4, qo=PTR[2], pos=PTR[4])
+    assert append(qos=256, **q) == zsa.ESHAPE
+    assert append(qos=768, **q) == zsa.ESHAPE
