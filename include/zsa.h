@@ -459,8 +459,11 @@ int zsa_paged_append(void* stream, const zsa_paged_kv* kv, const void* k, int64_
  *   out      [T, n_heads*head_dim], row stride out_stride; lse [n_heads, T]
  *            fp32 or NULL
  *   ws >= zsa_paged_attention_workspace_size(..., prefix_len 0)
- * bf16 or fp32, sums and softmax in fp32; head_dim 16, 32, 64 or 128. Up to
- * 2^30 rows times heads, and 2^30 cached rows a sequence.
+ * bf16 or fp32, scores, sums and softmax in fp32; head_dim 16, 32, 64 or 128.
+ * In bf16 with head_dim 32 and more a probability meets its value as one bf16
+ * number where a sequence (or a prefix) has many query rows, as in
+ * zsa_attention_with_scores, as two of 16 bits together where it has few: which,
+ * is up to the batch. Up to 2^30 rows times heads, and 2^30 cached rows a sequence.
  */
 int zsa_paged_attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride,
                         int32_t n_heads, int32_t causal, float scale, int32_t batch,
@@ -471,8 +474,11 @@ int zsa_paged_attention(void* stream, const zsa_paged_kv* kv, const void* q, int
 /* The same for sequences that share their first prefix_len rows: those are
  * cached once, in the pages prefix_pages [ceil(prefix_len / page_size)] int32
  * device, come before each sequence's own rows (table, kv_len and max_kv_len:
- * without them) and are seen by every new row. They are read once for the
- * whole batch. prefix_len 0 is zsa_paged_attention. */
+ * without them) and are seen by every new row. A long prefix is a job of its
+ * own for the query rows of the whole batch, which reads it once for every 256
+ * of them, or for every 16 where that stays small; one short enough that it is
+ * found in the caches is read with each sequence's rows. prefix_len 0 is
+ * zsa_paged_attention. */
 int zsa_prefix_attention(void* stream, const zsa_paged_kv* kv, const void* q, int64_t q_stride,
                          int32_t n_heads, int32_t causal, float scale, int32_t batch,
                          const int32_t* cu_host, const int32_t* cu_dev, const int32_t* kv_len,
