@@ -227,8 +227,8 @@ __device__ __forceinline__ const char* row_of_key(const PagedAttention& a, const
 // numbers whose sum has 16 bits: the matrix cores have the time. 32 packed rows
 // at a time (the 32-wide products) took as long where the bytes bound it and
 // longer elsewhere (8 of 128 on 1, 16 of up to 10000 rows 20.4, 16 at a time 19.6).
-// One row of 64 sequences of up to 4096, 32 heads of 128 on 8: 98 us and 5 for
-// the join, 5.4 TB/s in all; of 4 of up to 65536 156, 6.1 TB/s.
+// One row of 64 sequences of up to 4096, 32 heads of 128 on 8: 99 us and 5 for
+// the join, 5.4 TB/s in all; of 4 of up to 65536 157, 6.1 TB/s.
 template <int HD, int NW>
 struct FewShared {  // LDS of a group of NW waves
   static constexpr int HP = 17;  // merge row stride: [channel][row]
@@ -557,7 +557,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD <= 6
 //    to 32 keys, masked in the one step that holds them.
 //  * P is rounded to bf16 for the second product, as there: half a step of
 //    each probability, which the sums of many average out.
-// 4 x 1024 new rows over up to 8024, 32 heads of 128 on 8, 360 us, 1.06 PFLOP/s
+// 4 x 1024 new rows over up to 8024, 32 heads of 128 on 8, 350 us, 1.09 PFLOP/s
 // (the few-row kernel 751); 4 x 1024 over 8192, 32 of 64, 303 us, 0.91.
 template <int HD, int QB, int NW>
 struct ManyShared {
