@@ -194,18 +194,14 @@ __device__ __forceinline__ scalar_ids scalar(const int32_t* p) {
   return reinterpret_cast<scalar_ids>(reinterpret_cast<uintptr_t>(p));
 }
 
-// A key's row as it lies in the pool, for results that are computed again: key
-// j below `head` is row j of the common prefix, the others are the sequence's
-// own. Null where there is none: a page outside the pool, a prefix filled up.
-template <bool HEAD>
-__device__ __forceinline__ const char* row_of_key(const PagedAttention& a, const Span& sp, int head, int esize, int j) {
-  const bool first = HEAD && j < head;
-  const int i = HEAD && !first ? j - head : j;
-  const int page = i < (first ? a.head_len : sp.len) ? (first ? a.head_table : sp.table)[i >> a.at.shift] : -1;
-  return page < 0 || page >= a.at.n_pages
-             ? nullptr
-             : static_cast<const char*>(a.at.pool) + page * (a.at.page_stride * esize) +
-                   static_cast<uint32_t>(i & ((1 << a.at.shift) - 1)) * (2u * a.at.kvd * esize);
+// The values, but 2^120 in the place of larger ones, infinities and NaN (-2^120
+// of those below zero): as signed integers their bits are above the positive
+// numbers', as unsigned ones above the negative numbers'.
+__device__ __forceinline__ bf16x8_t bounded(bf16x8_t v) {
+  typedef int16_t i16x8 __attribute__((ext_vector_type(8)));
+  typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+  const i16x8 x = __builtin_elementwise_min(__builtin_bit_cast(i16x8, v), i16x8(int16_t{0x7b80}));
+  return __builtin_bit_cast(bf16x8_t, __builtin_elementwise_min(__builtin_bit_cast(u16x8, x), u16x8(uint16_t{0xfb80})));
 }
 
 // Workgroups of the few-row kernels: the (key/value head, sequence) pairs
@@ -224,7 +220,10 @@ __device__ __forceinline__ const char* row_of_key(const PagedAttention& a, const
 // page outside the pool. The transposed products leave a lane eight scores of
 // one row, keys 4 (l / 16) + r and those + 16, which are its operand of the
 // second product; V is read in that same order of keys. P meets V as two bf16
-// numbers whose sum has 16 bits: the matrix cores have the time. 32 packed rows
+// numbers whose sum has 16 bits: the matrix cores have the time. The second,
+// which is zero or below it as often as not, meets bounded values: an infinite
+// one is the first's to pass on (the second is up to 1 in size, and 32 of 2^120
+// stay a number). 32 packed rows
 // at a time (the 32-wide products) took as long where the bytes bound it and
 // longer elsewhere (8 of 128 on 1, 16 of up to 10000 rows 20.4, 16 at a time 19.6).
 // One row of 64 sequences of up to 4096, 32 heads of 128 on 8: 99 us and 5 for
@@ -406,6 +405,8 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
         const float p0 = __builtin_amdgcn_exp2f((s[t][r] - m_use) * scale_log2);
         const float p1 = __builtin_amdgcn_exp2f((s[t][r + 1] - m_use) * scale_log2);
         l_run += p0 + p1;
+        s[t][r] = p0;
+        s[t][r + 1] = p1;
         const uint32_t w = pack_bf16x2(p0, p1);
         hi[2 * t + (r >> 1)] = w;
         lo[2 * t + (r >> 1)] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u));
@@ -416,60 +417,42 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     asm volatile("" : "+s"(nx0), "+s"(nx1));  // here: scalar loads under way make every wait for LDS one for all
     __builtin_amdgcn_sched_barrier(0);
-    bf16x8_t vf[CT];
+    // A value that is not finite must not reach a row that does not see its
+    // key, through the product with its zero probability: where the tile holds
+    // hidden keys and such values, it goes through the vector ALU, key by key.
+    bool odd = false;
+    if ((!HEAD || j0 >= head) && lim0 < min(j0 + 32, end)) {
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-      vf[ct] = __builtin_bit_cast(bf16x8_t, lds_read_columns(mine + vaddr[ct], mine + vaddr[ct] + 16 * RB));
-    __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < 2 * NL; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(mine + HALF + i * 1024 + lane * 16);
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-      o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[ct], __builtin_bit_cast(bf16x8_t, hi), o[ct], 0, 0, 0);
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-      o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[ct], __builtin_bit_cast(bf16x8_t, lo), o[ct], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) load(jn, pg0, pg1, lds0 + HALF, vcol, voff);
-  }
-  l_run = quarter_swap_sum(l_run);
-  // A value that is not finite leaves a NaN where its key is hidden, through the
-  // product with a probability of zero, and an infinite one that is seen does
-  // where the two numbers of its probability have two signs, or one is zero.
-  // Rows with such results are computed again, the wave's keys one by one with
-  // their probabilities in fp32; a NaN score leaves one in any case.
-  bool odd = false;
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) odd |= o[ct][r] != o[ct][r];
-  if (__builtin_amdgcn_ballot_w64(odd && l_run == l_run) != 0) {
-    const float m_use = m_run == -INFINITY ? 0.f : m_run;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) o[ct] = zero;
-#pragma unroll 1
-    for (int j = k0 + wave * 32; j < kend; j += 32 * NW) {
-      f32x4_t s[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const char* kr = row_of_key<HEAD>(a, sp, head, 2, j + 16 * t + l16);
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          u32x4 k = {0u, 0u, 0u, 0u};
-          if (kr != nullptr) k = *reinterpret_cast<const u32x4*>(kr + kcol + kk * 64 + quarter * 16);
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k), qf[kk], kk == 0 ? zero : s[t], 0, 0, 0);
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[t][r] = __builtin_amdgcn_exp2f((s[t][r] - m_use) * scale_log2);
+        for (int e = 0; e < 4; ++e)
+          odd |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
       }
+      odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+    }
+    if (!odd) {
+      bf16x8_t vf[CT];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+        vf[ct] = __builtin_bit_cast(bf16x8_t, lds_read_columns(mine + vaddr[ct], mine + vaddr[ct] + 16 * RB));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+        o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[ct], __builtin_bit_cast(bf16x8_t, hi), o[ct], 0, 0, 0);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+        o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bounded(vf[ct]), __builtin_bit_cast(bf16x8_t, lo), o[ct], 0, 0, 0);
+    } else {
 #pragma unroll
       for (int kk = 0; kk < 32; ++kk) {
-        // key j + kk: register kk % 4 of tile kk / 16, lane quarter (kk / 4) % 4
+        // key j0 + kk: register kk % 4 of tile kk / 16, lane quarter (kk / 4) % 4
         const float p = __shfl(s[kk >> 4][kk & 3], l16 + 16 * ((kk >> 2) & 3), 64);
-        const char* vr = j + kk < lim ? row_of_key<HEAD>(a, sp, head, 2, j + kk) : nullptr;
-        if (vr != nullptr) {
+        if (j0 + kk < lim) {
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
-            const uint2 w = *reinterpret_cast<const uint2*>(vr + vcol + (ct * 16 + 4 * quarter) * 2);
+            const int c = ct * 16 + 4 * quarter;
+            const uint2 w = *reinterpret_cast<const uint2*>(mine + HALF + kk * RB + (((c >> 3) ^ vsw(kk)) << 4) + (c & 7) * 2);
             o[ct][0] = fmaf(p, __uint_as_float(w.x << 16), o[ct][0]);
             o[ct][1] = fmaf(p, __uint_as_float(w.x & 0xffff0000u), o[ct][1]);
             o[ct][2] = fmaf(p, __uint_as_float(w.y << 16), o[ct][2]);
@@ -478,7 +461,11 @@ __device__ __forceinline__ void few_rows(const PagedAttention& a, int block, boo
         }
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) load(jn, pg0, pg1, lds0 + HALF, vcol, voff);
   }
+  l_run = quarter_swap_sum(l_run);
   __syncthreads();  // every wave is past its tiles
   float* so = reinterpret_cast<float*>(smem);
   if (quarter == 0) {
@@ -882,6 +869,14 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
           for (int r = 0; r < 16; ++r) odd |= o[qb][ct][r] != o[qb][ct][r];
     }
     if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+      auto row_of = [&](int j) {  // row j's keys, or null
+        const bool first = HEAD && j < head;
+        const int i = first ? j : j - head;
+        const int page = i < (first ? a.head_len : sp.len) ? (first ? a.head_table : sp.table)[i >> a.at.shift] : -1;
+        return page < 0 || page >= a.at.n_pages
+                   ? nullptr
+                   : pool + page * (a.at.page_stride * 2) + static_cast<uint32_t>(i & ((1 << a.at.shift) - 1)) * rowb + g * RB;
+      };
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
         float m = kNoReference, l = 0.f;  // of the raw scores
@@ -890,12 +885,12 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[qb][ct][r] = 0.f;
         for (int j0 = k0; j0 < wlast; j0 += 32) {
-          const char* kr = row_of_key<HEAD>(a, sp, head, 2, j0 + l32);
+          const char* kr = row_of(j0 + l32);
           f32x16_t s = zero;
 #pragma unroll
           for (int kk = 0; kk < KK; ++kk) {
             u32x4 k = {0u, 0u, 0u, 0u};
-            if (kr != nullptr) k = *reinterpret_cast<const u32x4*>(kr + g * RB + kk * 32 + half * 16);
+            if (kr != nullptr) k = *reinterpret_cast<const u32x4*>(kr + kk * 32 + half * 16);
             s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), qf[qb][kk], s, 0, 0, 0);
           }
           float mx = m;
@@ -924,13 +919,13 @@ __device__ __forceinline__ void many_rows(const PagedAttention& a, int block, Ma
           for (int kk = 0; kk < 32; ++kk) {
             // key j0 + kk: register (kk / 8) * 4 + kk % 4 of lane half (kk / 4) % 2
             const float p = __shfl(s[(kk >> 3) * 4 + (kk & 3)], l32 + 32 * ((kk >> 2) & 1), 64);
-            const char* vr = j0 + kk < lim[qb] ? row_of_key<HEAD>(a, sp, head, 2, j0 + kk) : nullptr;
+            const char* vr = j0 + kk < lim[qb] ? row_of(j0 + kk) : nullptr;
             if (vr != nullptr) {
 #pragma unroll
               for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
-                  const uint2 w = *reinterpret_cast<const uint2*>(vr + g * RB + rowb / 2 + (ct * 32 + 2 * r + 4 * half) * 2);
+                  const uint2 w = *reinterpret_cast<const uint2*>(vr + rowb / 2 + (ct * 32 + 2 * r + 4 * half) * 2);
                   o[qb][ct][r] = fmaf(p, __uint_as_float(w.x << 16), o[qb][ct][r]);
                   o[qb][ct][r + 1] = fmaf(p, __uint_as_float(w.x & 0xffff0000u), o[qb][ct][r + 1]);
                   o[qb][ct][r + 2] = fmaf(p, __uint_as_float(w.y << 16), o[qb][ct][r + 2]);
@@ -1229,9 +1224,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     asm volatile("" : "+s"(nx0), "+s"(nx1));  // here: scalar loads under way make every wait for LDS one for all
     __builtin_amdgcn_sched_barrier(0);
-    // A value that is not finite must not reach a row that does not see its
-    // key, through the product with its zero probability: where the tile holds
-    // hidden keys and such values, it goes through the vector ALU, key by key.
+    // hidden keys' values that are not finite: key by key (few_rows)
     bool odd = false;
     if ((!HEAD || j0 >= head) && lim0 < min(j0 + 32, end)) {
 #pragma unroll

@@ -61,6 +61,19 @@ def test_infinite_values(dtype, hd, new, lens, prefix, causal):
         assert np.isposinf(ref[:, 9]).all() and np.isneginf(ref[:, 3 * hd + 9]).all()
 
 
+@pytest.mark.parametrize("dtype,hd", TYPES)
+@pytest.mark.parametrize("new,lens,prefix", FEW)
+def test_whole_channels_of_infinities(dtype, hd, new, lens, prefix):
+    # Many infinities in one sum, whose probabilities' second numbers have any
+    # sign; beside them channels of 2^110, finite in all sums.
+    b = Batch(dtype, 4, 2, hd, 16, new, lens, prefix, seed=hd + new[0])
+    values = b.pool[..., 2 * hd:]
+    values[..., 2], values[..., hd + 6] = float("inf"), -float("inf")
+    values[..., 3], values[..., 4] = 2.0 ** 110, -2.0 ** 110
+    ref = check_values(b, True)
+    assert np.isposinf(ref[0, 2]) and np.isneginf(ref[0, 3 * hd + 6]) and np.isfinite(ref[0, 3])
+
+
 def margins(b, causal):
     """Of every row and head: how far its largest score is above the next."""
     pool, q, G, kvd = f64(b.pool), f64(b.q).reshape(b.cu[-1], b.H, b.hd), b.H // b.kv, b.kv * b.hd
