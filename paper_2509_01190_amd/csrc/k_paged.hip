@@ -544,7 +544,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD <= 6
 //    to 32 keys, masked in the one step that holds them.
 //  * P is rounded to bf16 for the second product, as there: half a step of
 //    each probability, which the sums of many average out.
-// 4 x 1024 new rows over up to 8024, 32 heads of 128 on 8, 350 us, 1.09 PFLOP/s
+// 4 x 1024 new rows over up to 8024, 32 heads of 128 on 8, 361 us, 1.06 PFLOP/s
 // (the few-row kernel 751); 4 x 1024 over 8192, 32 of 64, 303 us, 0.91.
 template <int HD, int QB, int NW>
 struct ManyShared {
